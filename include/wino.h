@@ -363,6 +363,89 @@ int wino_i8_input_transform(const void *x, void *Vq, float *dV, int N, int C, in
 int wino_i8_batched_gemm(const void *Uq, const float *dU, const void *Vq, const float *dV, float *M,
                          int K, int C, int T, int block_shape, void *stream);
 
+/*
+ * The operators of the transformer block that stands between two residual blocks of a Stable-Diffusion UNet, on channel-last
+ * activations (a [N][H][W][C] tensor is M = N*H*W rows of C features as it stands): matrix products with bias, activation and
+ * residual in their epilogue, the gated feed-forward product, and attention to an encoder's states, each with its backward pass.
+ * The paper defines none of them; the textbook definitions apply.  Storage types, accumulation, streams, alignment of pointers,
+ * determinism and errors as above.  Sums, softmax statistics and bias gradients are fp32; a result is rounded once to `dtype`.
+ * Where a call needs more than one kernel, what passes between them is in fp32, except the gradient of the pre-activations (dz,
+ * [du | dg] below) and the softmax weights and their gradients inside the attention kernels, which are operands of the next matrix
+ * product and are rounded to `dtype` for it.  Calls with two-byte types take the hardware's exponential and reciprocal, fp32 calls
+ * the correctly scaled functions.
+ * "Overlap" is taken from the first to the last byte of a tensor, gaps between strided rows included.
+ * A workspace belongs to one call at a time: calls on different streams, and graphs that may run at the same time, need one each.
+ * Sizes with no effect on it may be anything; the *_workspace_bytes calls return 0 where none is needed (then workspace may be NULL)
+ * and for bad arguments.
+ */
+/* act(z): z;  SiLU z/(1+exp(-z));  GELU z*(1+erf(z/sqrt 2))/2;  GELU with tanh z*(1+tanh(sqrt(2/pi)*(z+0.044715 z^3)))/2 */
+typedef enum wino_act { WINO_ACT_NONE = 0, WINO_ACT_SILU = 1, WINO_ACT_GELU = 2, WINO_ACT_GELU_TANH = 3 } wino_act;
+
+/*
+ *     y[m][n] = act( sum_k x[m][k] * w[n][k] + bias[n] ) + residual[m][n]
+ *   x[M][K], residual[M][N], y[M][N]: rows of ldx, ldr, ldy elements (at least as many as they hold), w[N][K] contiguous, bias fp32 [N].
+ *   bias and residual may be NULL; residual may be y itself (with ldr = ldy), nothing else may overlap y.
+ */
+size_t wino_linear_workspace_bytes(int M, int N, int K, int dtype, int act);
+int wino_linear(const void *x, const void *w, const float *bias, const void *residual, void *y,
+                int M, int N, int K, long long ldx, long long ldr, long long ldy, int dtype, int act,
+                void *workspace, size_t workspace_bytes, void *stream);
+/*
+ * Its gradients for dy[M][N] (rows of lddy elements), from the inputs of the forward call; nothing has to be kept but those:
+ *     dz = dy * act'(x w^T + bias);   dx[M][K] = dz w;   dw[N][K] = dz^T x;   dbias[N] = sum_m dz[m]   (fp32);   d residual = dy
+ *   dx (rows of lddx elements), dw (contiguous) and dbias are overwritten; each may be NULL, then it is not computed.  Outputs must
+ *   not overlap inputs.
+ */
+size_t wino_linear_backward_workspace_bytes(int M, int N, int K, int dtype, int act);
+int wino_linear_backward(const void *x, const void *w, const float *bias, const void *dy, void *dx, void *dw, float *dbias,
+                         int M, int N, int K, long long ldx, long long lddy, long long lddx, int dtype, int act,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The gated feed-forward product, both projections, the activation and the product in one kernel:
+ *     u = x wu^T + bu,   g = x wg^T + bg,   h = u * act(g)          w[2N][K] = wu above wg, bias fp32 [2N] = bu, bg (or NULL)
+ *   x[M][K], h[M][N]: rows of ldx, ldh elements.  (The block's last product is a wino_linear with the residual.)
+ * Backward, for dh[M][N] (rows of lddh elements), with u and g made again from x:
+ *     du = dh * act(g),  dg = dh * u * act'(g);   dx = du wu + dg wg;   dw[2N][K] = [du | dg]^T x;   dbias[2N] = column sums
+ */
+size_t wino_glu_workspace_bytes(int M, int N, int K, int dtype, int act);
+int wino_glu(const void *x, const void *w, const float *bias, void *h, int M, int N, int K, long long ldx, long long ldh,
+             int dtype, int act, void *workspace, size_t workspace_bytes, void *stream);
+size_t wino_glu_backward_workspace_bytes(int M, int N, int K, int dtype, int act);
+int wino_glu_backward(const void *x, const void *w, const float *bias, const void *dh, void *dx, void *dw, float *dbias,
+                      int M, int N, int K, long long ldx, long long lddh, long long lddx, int dtype, int act,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Attention of Sq queries to Skv keys and values of another tensor (an encoder's states), or of the same one:
+ *     s_ij = scale * sum_d q[b][i][h][d] * k[b][j][h'][d],   p_i = softmax over the valid j,   o[b][i][h] = sum_j p_ij v[b][j][h']
+ *   with h' = h / (H / Hkv): neighbouring query heads share a key head.  Key j of batch row b is valid if j < kv_len[b] and
+ *   key_mask[b][j] != 0 (device arrays, either may be NULL; a length outside [0, Skv] counts as the nearer end).  A batch row without
+ *   a valid key gives o = 0 and lse = -infinity.  What k and v hold at other keys is never read.
+ *   lse[b][h][i] = log sum_j exp(s_ij), fp32 [B][H][Sq]; NULL where no backward pass follows.
+ * Tensors are [batch][position][head][D] with strides of their own in elements (a slice of a packed q,k,v product is read in place);
+ * D is contiguous, a multiple of 8, at most 256 (fp32: 160).  Strides are not negative and multiples of 16 bytes; those of outputs
+ * are positive and must not let positions overlap.  scale > 0.  Outputs must not overlap inputs.
+ */
+typedef struct wino_tensor { void *data; long long stride_b, stride_s, stride_h; } wino_tensor;
+typedef struct wino_attention_args {
+    int B, Sq, Skv, H, Hkv, D;
+    int dtype;
+    float scale;
+    wino_tensor q, k, v, o;
+    float *lse;
+    const int *kv_len;                 /* device, [B], or NULL       */
+    const unsigned char *key_mask;     /* device, [B][Skv], or NULL  */
+    wino_tensor d_o, dq, dk, dv;       /* backward pass only         */
+} wino_attention_args;
+size_t wino_attention_workspace_bytes(int B, int Sq, int Skv, int H, int Hkv, int D, int dtype);
+int wino_attention(const wino_attention_args *a, void *workspace, size_t workspace_bytes, void *stream);
+/* Gradients of q, k and v for d_o, from the inputs, o and lse of the forward call (same scale, lengths and mask):
+ *     ds_ij = p_ij * (d_o_i . v_j - d_o_i . o_i),   dq = scale * ds k,   dk = scale * ds^T q,   dv = p^T d_o
+ * dk and dv are summed over the query heads that share a key head and are zero at keys that are not valid. */
+size_t wino_attention_backward_workspace_bytes(int B, int Sq, int Skv, int H, int Hkv, int D, int dtype);
+int wino_attention_backward(const wino_attention_args *a, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

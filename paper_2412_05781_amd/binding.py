@@ -22,6 +22,7 @@ WINO_ERR_ALIGN, WINO_ERR_WORKSPACE, WINO_ERR_ALIAS, WINO_ERR_HIP, WINO_ERR_LAYOU
 WINO_F32, WINO_F16, WINO_BF16 = 0, 1, 2
 WINO_AUTO, WINO_DIRECT, WINO_F2, WINO_F4, WINO_FUSED_F2, WINO_FUSED_F4 = 0, 1, 2, 4, 12, 14
 WINO_NCHW, WINO_NHWC = 0, 1
+WINO_ACT_NONE, WINO_ACT_SILU, WINO_ACT_GELU, WINO_ACT_GELU_TANH = 0, 1, 2, 3
 
 DTYPE_OF = {torch.float32: WINO_F32, torch.float16: WINO_F16, torch.bfloat16: WINO_BF16}
 TORCH_OF = {WINO_F32: torch.float32, WINO_F16: torch.float16, WINO_BF16: torch.bfloat16}
@@ -37,6 +38,9 @@ EXPORTS = [
     "wino_fused_gemm_output", "wino_batched_gemm_shape", "wino_static_scratch_bytes", "wino_conv2d_static",
     "wino_i8_filter_bytes", "wino_i8_filter_transform", "wino_i8_workspace_bytes", "wino_i8_conv2d",
     "wino_i8_input_transform", "wino_i8_batched_gemm", "wino_fused_f4_gemm_output",
+    "wino_linear_workspace_bytes", "wino_linear", "wino_linear_backward_workspace_bytes", "wino_linear_backward",
+    "wino_glu_workspace_bytes", "wino_glu", "wino_glu_backward_workspace_bytes", "wino_glu_backward",
+    "wino_attention_workspace_bytes", "wino_attention", "wino_attention_backward_workspace_bytes", "wino_attention_backward",
 ]
 
 
@@ -49,6 +53,17 @@ class wino_fusion(ctypes.Structure):
     _fields_ = [("gn_stats", ctypes.c_void_p), ("gn_gamma", ctypes.c_void_p), ("gn_beta", ctypes.c_void_p),
                 ("gn_groups", ctypes.c_int), ("addvec", ctypes.c_void_p), ("residual", ctypes.c_void_p),
                 ("upsample", ctypes.c_int), ("product_fp16", ctypes.c_int)]
+
+
+class wino_tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_longlong), ("stride_s", ctypes.c_longlong), ("stride_h", ctypes.c_longlong)]
+
+
+class wino_attention_args(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("Sq", ctypes.c_int), ("Skv", ctypes.c_int), ("H", ctypes.c_int), ("Hkv", ctypes.c_int), ("D", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("scale", ctypes.c_float), ("q", wino_tensor), ("k", wino_tensor), ("v", wino_tensor), ("o", wino_tensor),
+                ("lse", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("key_mask", ctypes.c_void_p),
+                ("d_o", wino_tensor), ("dq", wino_tensor), ("dk", wino_tensor), ("dv", wino_tensor)]
 
 
 class WinoError(RuntimeError):
@@ -124,6 +139,19 @@ def lib() -> ctypes.CDLL:
         L.wino_igemm_workspace_bytes.restype = sz; L.wino_igemm_workspace_bytes.argtypes = [i] * 9
         L.wino_igemm_conv2d.restype = i
         L.wino_igemm_conv2d.argtypes = [vp, vp, vp, vp, i, i, i, i, i, i, i, i, i, vp, sz, vp]
+        ll = ctypes.c_longlong
+        for name in ("linear", "linear_backward", "glu", "glu_backward"):
+            f = getattr(L, f"wino_{name}_workspace_bytes")
+            f.restype = sz; f.argtypes = [i] * 5
+        L.wino_linear.restype = i; L.wino_linear.argtypes = [vp] * 5 + [i] * 3 + [ll] * 3 + [i, i, vp, sz, vp]
+        L.wino_linear_backward.restype = i; L.wino_linear_backward.argtypes = [vp] * 7 + [i] * 3 + [ll] * 3 + [i, i, vp, sz, vp]
+        L.wino_glu.restype = i; L.wino_glu.argtypes = [vp] * 4 + [i] * 3 + [ll] * 2 + [i, i, vp, sz, vp]
+        L.wino_glu_backward.restype = i; L.wino_glu_backward.argtypes = [vp] * 7 + [i] * 3 + [ll] * 3 + [i, i, vp, sz, vp]
+        for name in ("attention", "attention_backward"):
+            f = getattr(L, f"wino_{name}_workspace_bytes")
+            f.restype = sz; f.argtypes = [i] * 7
+            f = getattr(L, f"wino_{name}")
+            f.restype = i; f.argtypes = [ctypes.POINTER(wino_attention_args), vp, sz, vp]
         _lib = L
     return _lib
 
@@ -605,7 +633,231 @@ def wino_i8_batched_gemm(Uq: torch.Tensor, dU: torch.Tensor, Vq: torch.Tensor, d
     return M
 
 
+# ---- operators of a transformer block -----------------------------------------------------------
+def _on_one_device(stream, first, *others):
+    """Every tensor lives on `first`'s GPU, and that is the current one unless a stream is named (kernels go where the stream is)."""
+    d = first.get_device()
+    if d < 0:
+        raise ValueError("tensors must live on a GPU")
+    for t in others:
+        if t is not None and t.get_device() != d:
+            raise ValueError("tensors live on different devices")
+    if (_current_device() if stream is None else stream.device_index) != d:
+        raise ValueError(f"tensors live on GPU {d}, which is not the one the call runs on")
+
+
+def _rows(t: torch.Tensor, name: str, rows: int, cols: int, dtype) -> int:
+    """The row stride of a [rows, cols] tensor whose rows are contiguous."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype != dtype:
+        raise ValueError(f"{name} must be [{rows}, {cols}] of {dtype}")
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.stride(0) if rows > 1 else cols
+
+
+def _weights(x, w, bias, halves: int):
+    """(M, N, K, dtype code) of x[M,K], w[halves*N,K] and bias[halves*N]."""
+    dt = DTYPE_OF.get(x.dtype)
+    if dt is None or x.dim() != 2 or w.dim() != 2 or w.dtype != x.dtype or w.shape[1] != x.shape[1] or w.shape[0] % halves or not w.is_contiguous():
+        raise ValueError("x must be [M, K] and w a contiguous [N, K] (gated: [2N, K]) of the same storage type")
+    if bias is not None and (bias.dtype != torch.float32 or bias.numel() != w.shape[0] or not bias.is_contiguous()):
+        raise ValueError("bias must be a contiguous fp32 tensor with one element per row of w")
+    return x.shape[0], w.shape[0] // halves, x.shape[1], dt
+
+
+def _ws(workspace):
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def wino_linear_workspace_bytes(M, N, K, dtype, act=WINO_ACT_NONE) -> int:
+    return lib().wino_linear_workspace_bytes(M, N, K, dtype, act)
+
+
+def wino_linear_backward_workspace_bytes(M, N, K, dtype, act=WINO_ACT_NONE) -> int:
+    return lib().wino_linear_backward_workspace_bytes(M, N, K, dtype, act)
+
+
+def wino_glu_workspace_bytes(M, N, K, dtype, act) -> int:
+    return lib().wino_glu_workspace_bytes(M, N, K, dtype, act)
+
+
+def wino_glu_backward_workspace_bytes(M, N, K, dtype, act) -> int:
+    return lib().wino_glu_backward_workspace_bytes(M, N, K, dtype, act)
+
+
+def wino_linear(x, w, bias, y, act: int = WINO_ACT_NONE, residual=None, workspace=None, stream=None):
+    """y[M,N] = act(x[M,K] w[N,K]^T + bias) + residual; rows of x, y and residual may be strided, residual may be y."""
+    M, N, K, dt = _weights(x, w, bias, 1)
+    ldx, ldy = _rows(x, "x", M, K, x.dtype), _rows(y, "y", M, N, x.dtype)
+    ldr = ldy if residual is None else _rows(residual, "residual", M, N, x.dtype)
+    _on_one_device(stream, x, w, bias, y, residual, workspace)
+    ws, n = _ws(workspace)
+    _check(lib().wino_linear(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), y.data_ptr(), M, N, K, ldx, ldr, ldy, dt, act, ws, n,
+                             _stream(stream)), "wino_linear")
+    return y
+
+
+def _product_backward(name, halves, x, w, bias, dy, dx, dw, dbias, act, workspace, stream):
+    M, N, K, dt = _weights(x, w, bias, halves)
+    ldx, lddy = _rows(x, "x", M, K, x.dtype), _rows(dy, "the output's gradient", M, N, x.dtype)
+    lddx = K if dx is None else _rows(dx, "dx", M, K, x.dtype)
+    if dw is not None and (dw.shape != w.shape or dw.dtype != x.dtype or not dw.is_contiguous()):
+        raise ValueError("dw must be contiguous with the shape and type of w")
+    if dbias is not None and (dbias.dtype != torch.float32 or dbias.numel() != halves * N or not dbias.is_contiguous()):
+        raise ValueError("dbias must be a contiguous fp32 tensor with one element per row of w")
+    _on_one_device(stream, x, w, bias, dy, dx, dw, dbias, workspace)
+    ws, n = _ws(workspace)
+    _check(getattr(lib(), name)(x.data_ptr(), w.data_ptr(), _ptr(bias), dy.data_ptr(), _ptr(dx), _ptr(dw), _ptr(dbias), M, N, K, ldx, lddy, lddx,
+                                dt, act, ws, n, _stream(stream)), name)
+    return dx, dw, dbias
+
+
+def wino_linear_backward(x, w, bias, dy, dx, dw, dbias, act: int = WINO_ACT_NONE, workspace=None, stream=None):
+    """Gradients of wino_linear for dy; dx, dw and dbias are written where they are not None (the residual's gradient is dy)."""
+    return _product_backward("wino_linear_backward", 1, x, w, bias, dy, dx, dw, dbias, act, workspace, stream)
+
+
+def wino_glu(x, w, bias, h, act: int = WINO_ACT_GELU, workspace=None, stream=None):
+    """h[M,N] = (x wu^T + bu) * act(x wg^T + bg) with w[2N,K] = wu above wg and bias[2N] = bu, bg."""
+    M, N, K, dt = _weights(x, w, bias, 2)
+    ldx, ldh = _rows(x, "x", M, K, x.dtype), _rows(h, "h", M, N, x.dtype)
+    _on_one_device(stream, x, w, bias, h, workspace)
+    ws, n = _ws(workspace)
+    _check(lib().wino_glu(x.data_ptr(), w.data_ptr(), _ptr(bias), h.data_ptr(), M, N, K, ldx, ldh, dt, act, ws, n, _stream(stream)), "wino_glu")
+    return h
+
+
+def wino_glu_backward(x, w, bias, dh, dx, dw, dbias, act: int = WINO_ACT_GELU, workspace=None, stream=None):
+    """Gradients of wino_glu for dh; dx, dw and dbias are written where they are not None."""
+    return _product_backward("wino_glu_backward", 2, x, w, bias, dh, dx, dw, dbias, act, workspace, stream)
+
+
+def wino_attention_workspace_bytes(B, Sq, Skv, H, Hkv, D, dtype) -> int:
+    return lib().wino_attention_workspace_bytes(B, Sq, Skv, H, Hkv, D, dtype)
+
+
+def wino_attention_backward_workspace_bytes(B, Sq, Skv, H, Hkv, D, dtype) -> int:
+    return lib().wino_attention_backward_workspace_bytes(B, Sq, Skv, H, Hkv, D, dtype)
+
+
+def _heads(field, t, name, shape, dtype):
+    if t.shape != shape or t.dtype != dtype or (t.stride(3) != 1 and shape[3] > 1):
+        raise ValueError(f"{name} must be {list(shape)} of {dtype} with contiguous channels")
+    field.data = t.data_ptr()
+    field.stride_b, field.stride_s, field.stride_h, _ = t.stride()
+
+
+def _attention(q, k, v, o, lse, kv_len, key_mask, scale):
+    if q.dim() != 4 or k.dim() != 4 or q.dtype not in DTYPE_OF:
+        raise ValueError("q must be [B, Sq, H, D] and k, v [B, Skv, Hkv, D] in one of the storage types")
+    B, Sq, H, D = q.shape
+    _, Skv, Hkv, _ = kshape = k.shape
+    a = wino_attention_args(B, Sq, Skv, H, Hkv, D, DTYPE_OF[q.dtype], D ** -0.5 if scale is None else scale)
+    _heads(a.q, q, "q", q.shape, q.dtype)
+    _heads(a.k, k, "k", (B, Skv, Hkv, D), q.dtype)
+    _heads(a.v, v, "v", kshape, q.dtype)
+    _heads(a.o, o, "o", q.shape, q.dtype)
+    if lse is not None:
+        if lse.dtype != torch.float32 or lse.shape != (B, H, Sq) or not lse.is_contiguous():
+            raise ValueError("lse must be a contiguous fp32 tensor [B, H, Sq]")
+        a.lse = lse.data_ptr()
+    if kv_len is not None:
+        if kv_len.dtype != torch.int32 or kv_len.shape != (B,) or not kv_len.is_contiguous():
+            raise ValueError("kv_len must be a contiguous int32 tensor [B]")
+        a.kv_len = kv_len.data_ptr()
+    if key_mask is not None:
+        if key_mask.dtype not in (torch.uint8, torch.bool) or key_mask.shape != (B, Skv) or not key_mask.is_contiguous():
+            raise ValueError("key_mask must be a contiguous uint8 or bool tensor [B, Skv]")
+        a.key_mask = key_mask.data_ptr()
+    return a
+
+
+def wino_attention(q, k, v, o, lse=None, kv_len=None, key_mask=None, scale=None, workspace=None, stream=None):
+    """o[B,Sq,H,D] = softmax(scale q k^T) v over the valid keys; k, v [B,Skv,Hkv,D]; any strides with contiguous channels.
+    scale None: 1 / sqrt(D).  lse [B,H,Sq] fp32 is written where given; a backward pass needs it."""
+    a = _attention(q, k, v, o, lse, kv_len, key_mask, scale)
+    _on_one_device(stream, q, k, v, o, lse, kv_len, key_mask, workspace)
+    ws, n = _ws(workspace)
+    _check(lib().wino_attention(ctypes.byref(a), ws, n, _stream(stream)), "wino_attention")
+    return o
+
+
+def wino_attention_backward(q, k, v, o, lse, do, dq, dk, dv, kv_len=None, key_mask=None, scale=None, workspace=None, stream=None):
+    """Gradients of q, k and v for do, from the inputs and results (o, lse) of wino_attention."""
+    a = _attention(q, k, v, o, lse, kv_len, key_mask, scale)
+    _heads(a.d_o, do, "do", q.shape, q.dtype)
+    _heads(a.dq, dq, "dq", q.shape, q.dtype)
+    _heads(a.dk, dk, "dk", k.shape, q.dtype)
+    _heads(a.dv, dv, "dv", k.shape, q.dtype)
+    _on_one_device(stream, q, k, v, o, lse, do, dq, dk, dv, kv_len, key_mask, workspace)
+    ws, n = _ws(workspace)
+    _check(lib().wino_attention_backward(ctypes.byref(a), ws, n, _stream(stream)), "wino_attention_backward")
+    return dq, dk, dv
+
+
 # ---- convenience (allocation only) ------------------------------------------------------------
+def _scratch(nbytes, like):
+    return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+
+
+def linear(x, w, bias=None, act: int = WINO_ACT_NONE, residual=None):
+    """act(x w^T + bias) + residual over the last dimension of x, with the output and the workspace allocated here."""
+    x2, N = x.reshape(-1, x.shape[-1]), int(w.shape[0])
+    y = torch.empty((x2.shape[0], N), dtype=x.dtype, device=x.device)
+    ws = _scratch(wino_linear_workspace_bytes(x2.shape[0], N, x2.shape[1], DTYPE_OF[x.dtype], act), x)
+    return wino_linear(x2, w, bias, y, act, None if residual is None else residual.reshape(-1, N), ws).view(*x.shape[:-1], N)
+
+
+def linear_backward(x, w, bias, dy, act: int = WINO_ACT_NONE):
+    """(dx, dw, dbias) of `linear`."""
+    x2, N = x.reshape(-1, x.shape[-1]), int(w.shape[0])
+    dx, dw = torch.empty(x2.shape, dtype=x.dtype, device=x.device), torch.empty_like(w)
+    dbias = torch.empty(N, dtype=torch.float32, device=x.device)
+    ws = _scratch(wino_linear_backward_workspace_bytes(x2.shape[0], N, x2.shape[1], DTYPE_OF[x.dtype], act), x)
+    wino_linear_backward(x2, w, bias, dy.reshape(-1, N), dx, dw, dbias, act, ws)
+    return dx.view(x.shape), dw, dbias
+
+
+def glu(x, w, bias=None, act: int = WINO_ACT_GELU):
+    """(x wu^T + bu) * act(x wg^T + bg) over the last dimension of x."""
+    x2, N = x.reshape(-1, x.shape[-1]), int(w.shape[0]) // 2
+    h = torch.empty((x2.shape[0], N), dtype=x.dtype, device=x.device)
+    ws = _scratch(wino_glu_workspace_bytes(x2.shape[0], N, x2.shape[1], DTYPE_OF[x.dtype], act), x)
+    return wino_glu(x2, w, bias, h, act, ws).view(*x.shape[:-1], N)
+
+
+def glu_backward(x, w, bias, dh, act: int = WINO_ACT_GELU):
+    """(dx, dw, dbias) of `glu`."""
+    x2, N = x.reshape(-1, x.shape[-1]), int(w.shape[0]) // 2
+    dx, dw = torch.empty(x2.shape, dtype=x.dtype, device=x.device), torch.empty_like(w)
+    dbias = torch.empty(2 * N, dtype=torch.float32, device=x.device)
+    ws = _scratch(wino_glu_backward_workspace_bytes(x2.shape[0], N, x2.shape[1], DTYPE_OF[x.dtype], act), x)
+    wino_glu_backward(x2, w, bias, dh.reshape(-1, N), dx, dw, dbias, act, ws)
+    return dx.view(x.shape), dw, dbias
+
+
+def attention(q, k, v, kv_len=None, key_mask=None, scale=None, with_lse: bool = False):
+    """softmax(scale q k^T) v; with_lse: (o, lse), what attention_backward takes."""
+    (B, Sq, H, D), (_, Skv, Hkv, _) = q.shape, k.shape
+    o = torch.empty((B, Sq, H, D), dtype=q.dtype, device=q.device)
+    lse = torch.empty((B, H, Sq), dtype=torch.float32, device=q.device) if with_lse else None
+    ws = _scratch(wino_attention_workspace_bytes(B, Sq, Skv, H, Hkv, D, DTYPE_OF[q.dtype]), q)
+    wino_attention(q, k, v, o, lse, kv_len, key_mask, scale, ws)
+    return (o, lse) if with_lse else o
+
+
+def attention_backward(q, k, v, o, lse, do, kv_len=None, key_mask=None, scale=None):
+    """(dq, dk, dv) of `attention`."""
+    (B, Sq, H, D), (_, Skv, Hkv, _) = q.shape, k.shape
+    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    ws = _scratch(wino_attention_backward_workspace_bytes(B, Sq, Skv, H, Hkv, D, DTYPE_OF[q.dtype]), q)
+    return wino_attention_backward(q, k, v, o, lse, do, dq, dk, dv, kv_len, key_mask, scale, ws)
+
+
 def conv2d_i8(x: torch.Tensor, w: torch.Tensor, bias=None, layout: int = WINO_NCHW) -> torch.Tensor:
     """Quantise the transformed filter, allocate workspace and output, run the Winograd path with 8-bit integer U and V."""
     N, C, H, W = _unpack(x, layout)

@@ -1,0 +1,124 @@
+// LDS tiles of the attention kernels: rows of one head's channels, read along the row (scores: the reduction runs over channels) and across the
+// rows (products with the weights: the reduction runs over rows).
+//
+// 32x32 MFMA accumulators hold, in register r of lane l, row 8 (r / 4) + 4 (l / 32) + r % 4 and column l % 32.  Scores are formed with the streamed
+// rows in the accumulator's rows and the wave's own 32 rows in its columns, one per lane.  The weights of a lane are then, register by register, an
+// operand of the next product as they stand, if the other operand takes the streamed rows in the same order: element j of half h of step t is row
+// 16 t + 8 (j / 4) + 4 h + j % 4 for two-byte types, 8 t + 4 h + j for fp32.  Nothing is exchanged between lanes or passed through LDS.
+#pragma once
+#include "block_internal.h"
+#include "wino_mma.h"
+
+namespace wino {
+
+typedef short attn_s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) attn_s16x4_t attn_lds_s16x4_t;
+
+// DP: channels / 16, rounded up
+template <typename E, int DP> struct AttnTile {
+    static constexpr int ES = (int)sizeof(E);
+    static constexpr int NV = (DP + 1) / 2;                     // 32-channel blocks
+    static constexpr int KS = ES == 2 ? DP : 2 * DP;            // MFMA steps over the channels
+    static constexpr int CPR = 2 * KS;                          // 16-byte chunks of a row that a score reads
+    static constexpr int V = 16 / ES;                           // elements per chunk
+    static constexpr int ST = ES == 2 ? 2 : 4;                  // MFMA steps over 32 streamed rows
+    static constexpr int ROWS = 64;                             // streamed rows per tile
+    // Two-byte types: an odd multiple of 64 bytes, and the low bits of the chunk flipped by (row / 4) % 4: sixteen rows read at one chunk and four rows
+    // read at 64 neighbouring bytes both touch every bank once.  fp32: an odd number of chunks.
+    static constexpr int STRIDE = ES == 2 ? 64 * (NV | 1) : NV * 128 + 16;
+    static constexpr int BYTES = ROWS * STRIDE;
+    static constexpr int LOADS = (ROWS * CPR + 255) / 256;      // chunks per thread and tile
+
+    static __device__ __forceinline__ int at(int row, int chunk) {
+        return row * STRIDE + ((ES == 2 ? chunk ^ ((row >> 2) & 3) : chunk) << 4);
+    }
+    // row row0 + lane % 32, channels of step ks
+    static __device__ __forceinline__ u32x4_t along(const unsigned char* t, int row0, int ks, int lane) {
+        return *reinterpret_cast<const u32x4_t*>(t + at(row0 + (lane & 31), 2 * ks + (lane >> 5)));
+    }
+    // channel 32 dt + lane % 32, rows of step st from row0
+    static __device__ __forceinline__ u32x4_t across(const unsigned char* t, int row0, int st, int dt, int lane) {
+        const int half = lane >> 5;
+        u32x4_t f;
+        if constexpr (ES == 2) {
+            const int col = dt * 32 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int row = row0 + 16 * st + 8 * k + 4 * half + ((lane & 15) >> 2);
+                const attn_s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((attn_lds_s16x4_t*)(t + at(row, col >> 3) + ((col & 4) << 1)));
+                const uint2 w = __builtin_bit_cast(uint2, v);
+                f[2 * k] = w.x;
+                f[2 * k + 1] = w.y;
+            }
+        } else {
+            const int col = dt * 32 + (lane & 31);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<const uint32_t*>(t + at(row0 + 8 * st + 4 * half + j, col >> 2) + ((col & 3) << 2));
+        }
+        return f;
+    }
+    // step st of 32 weights in accumulator order
+    static __device__ __forceinline__ u32x4_t weights(const float16_t& p, int st) {
+        u32x4_t f;
+        if constexpr (ES == 2) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = pack2<E>(p[8 * st + 2 * j], p[8 * st + 2 * j + 1]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = __float_as_uint(p[4 * st + j]);
+        }
+        return f;
+    }
+};
+
+// The rows that a key head's queries are dealt with as: r = g * Sq + s for query head hk * G + g, so that heads which share keys share a tile.
+struct AttnRows {
+    int Sq, R;                       // R = G * Sq
+    __device__ __forceinline__ const unsigned char* at(const AttnTensor& t, int G, int b, int hk, int r, int es) const {
+        const int g = r / Sq, s = r - g * Sq;
+        return static_cast<const unsigned char*>(t.p) + ((long long)b * t.b + (long long)s * t.s + (long long)(hk * G + g) * t.h) * es;
+    }
+};
+
+// 16 bytes at channel c of a row, zero behind the head's D channels (D is a multiple of 8)
+template <typename E> __device__ __forceinline__ u32x4_t load_channels(const unsigned char* row, int c, int D) {
+    const u32x4_t zero = {0, 0, 0, 0};
+    return c < D ? *reinterpret_cast<const u32x4_t*>(row + c * (int)sizeof(E)) : zero;
+}
+
+// four channels of one row
+template <typename E> __device__ __forceinline__ void store_channels(unsigned char* row, int c, int D, const float* v) {
+    if (c >= D) return;
+    if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(row + c * 4) = make_float4(v[0], v[1], v[2], v[3]);
+    else *reinterpret_cast<uint2*>(row + c * 2) = make_uint2(pack2<E>(v[0], v[1]), pack2<E>(v[2], v[3]));
+}
+
+// Valid keys among the 64 from key0 on, one bit each: below the row's length and not masked.  Called by whole waves.
+__device__ __forceinline__ unsigned long long valid_keys(const AttnArgs& a, int b, int key0, int len) {
+    const int key = key0 + (int)(threadIdx.x & 63);
+    bool ok = key < len;
+    if (a.key_mask && ok) ok = a.key_mask[(long long)b * a.Skv + key] != 0;
+    return __ballot(ok);
+}
+__device__ __forceinline__ int key_count(const AttnArgs& a, int b) {
+    if (!a.kv_len) return a.Skv;
+    const int n = a.kv_len[b];
+    return n < 0 ? 0 : n < a.Skv ? n : a.Skv;
+}
+
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
+
+// channels / 16 as a compile-time number
+template <typename F> hipError_t with_channels(int D, F&& f) {
+    const int n = (D + 15) / 16;
+    if (n <= 2) return f(std::integral_constant<int, 2>());
+    if (n == 3) return f(std::integral_constant<int, 3>());
+    if (n == 4) return f(std::integral_constant<int, 4>());
+    if (n == 5) return f(std::integral_constant<int, 5>());
+    if (n == 6) return f(std::integral_constant<int, 6>());
+    if (n <= 8) return f(std::integral_constant<int, 8>());
+    if (n <= 10) return f(std::integral_constant<int, 10>());
+    return f(std::integral_constant<int, 16>());
+}
+
+}  // namespace wino

@@ -1,0 +1,272 @@
+// C-ABI boundary of the transformer-block operators: argument validation on the host, workspace carving, and the chains of launches.
+// Nothing here computes.
+#include "../../include/wino.h"
+#include "block_internal.h"
+
+#include <math.h>
+
+using namespace wino;
+
+namespace {
+
+inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+inline bool at16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool at4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+inline bool is_dtype(int d) { return d == WINO_F32 || d == WINO_F16 || d == WINO_BF16; }
+inline bool is_act(int a) { return a >= WINO_ACT_NONE && a <= WINO_ACT_GELU_TANH; }
+inline size_t bytes_of(int d) { return d == WINO_F32 ? 4 : 2; }
+
+// bytes from the first to behind the last element of `rows` rows of `cols`
+inline size_t extent(long long rows, long long ld, long long cols, size_t es) { return ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * es; }
+inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && x < y + nb && y < x + na;
+}
+inline bool ld_ok(long long ld, long long cols) { return ld >= cols && ld <= (1LL << 36); }
+
+// product out[M][N] = Q P^T in one launch or as ranges that are joined; `scratch` holds the ranges' sums
+size_t product_bytes(int M, int N, int K, int dt) {
+    const int n = gemm_ranges(M, N, K, dt);
+    return n == 1 ? 0 : up256((size_t)n * M * N * sizeof(float));
+}
+hipError_t product(int ep, bool pt, bool qt, const Operand& P, const Operand& Q, const GemmShape& g, Epilogue e, void* scratch, int dt, hipStream_t s) {
+    const int n = gemm_ranges(g.M, g.N, g.K, dt);
+    if (n == 1) return launch_gemm(ep, pt, qt, P, Q, g, e, 1, dt, s);
+    e.part = static_cast<float*>(scratch);
+    const hipError_t rc = launch_gemm(EP_PART, pt, qt, P, Q, g, e, n, dt, s);
+    return rc != hipSuccess ? rc : launch_join(e.part, n, g, e, dt, s);
+}
+
+// workspace of a backward pass over W output columns: dz, the column sums, the ranges' sums
+struct BackwardSpace { size_t dz, sums, parts, total; long long ld; int sum_rows; };
+BackwardSpace backward_space(int M, int W, int K, int dt, bool stored) {
+    BackwardSpace b;
+    b.ld = ((long long)W + 7) / 8 * 8;
+    b.dz = stored ? up256((size_t)M * b.ld * bytes_of(dt)) : 0;
+    b.sum_rows = stored ? gemm_sum_rows(M, dt) : column_sum_rows(M);
+    b.sums = up256((size_t)b.sum_rows * W * sizeof(float));
+    const size_t px = product_bytes(M, K, W, dt), pw = product_bytes(W, K, M, dt);
+    b.parts = px > pw ? px : pw;
+    b.total = b.dz + b.sums + b.parts;
+    return b;
+}
+
+// dx = dz w and dw = dz^T x
+int run_products(const void* x, long long ldx, const void* w, const void* dz, long long lddz, void* dx, long long lddx, void* dw, int M, int W, int K, void* scratch, int dt, hipStream_t s) {
+    Epilogue e;
+    if (dx) {
+        e.out = dx; e.ld_out = lddx;
+        if (product(EP_STORE, true, false, Operand{w, K}, Operand{dz, lddz}, GemmShape{M, K, W}, e, scratch, dt, s) != hipSuccess) return WINO_ERR_HIP;
+    }
+    if (dw) {
+        e.out = dw; e.ld_out = K;
+        if (product(EP_STORE, true, true, Operand{x, ldx}, Operand{dz, lddz}, GemmShape{W, K, M}, e, scratch, dt, s) != hipSuccess) return WINO_ERR_HIP;
+    }
+    return WINO_OK;
+}
+
+bool product_dims_ok(int M, int N, int K, int halves) {
+    if (M < 1 || N < 1 || K < 1 || N > (1 << 27)) return false;
+    const long long W = (long long)N * halves;
+    return gemm_dims_ok(M, W, K) && gemm_dims_ok(M, K, W) && gemm_dims_ok(W, K, M);
+}
+
+// one call for both backward passes: `halves` rows of w per output column
+int products_backward(const void* x, const void* w, const float* bias, const void* dy, void* dx, void* dw, float* dbias, int M, int N, int K, long long ldx,
+                      long long lddy, long long lddx, int dt, int act, int halves, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!x || !w || !dy || (!dx && !dw && !dbias)) return WINO_ERR_NULL;
+    if (!is_dtype(dt)) return WINO_ERR_DTYPE;
+    if (!is_act(act)) return WINO_ERR_VARIANT;
+    if (!product_dims_ok(M, N, K, halves) || !ld_ok(ldx, K) || !ld_ok(lddy, N) || (dx && !ld_ok(lddx, K))) return WINO_ERR_DIM;
+    if (!at16(x) || !at16(w) || !at16(dy) || !at16(dx) || !at16(dw) || !at4(bias) || !at4(dbias)) return WINO_ERR_ALIGN;
+    const int W = N * halves;
+    const size_t es = bytes_of(dt);
+    const struct { const void* p; size_t n; } in[4] = {{x, extent(M, ldx, K, es)}, {w, (size_t)W * K * es}, {dy, extent(M, lddy, N, es)}, {bias, (size_t)W * 4}},
+                                              out[3] = {{dx, dx ? extent(M, lddx, K, es) : 0}, {dw, (size_t)W * K * es}, {dbias, (size_t)W * 4}};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < 4; ++j) if (overlap(out[i].p, out[i].n, in[j].p, in[j].n)) return WINO_ERR_ALIAS;
+        for (int j = 0; j < i; ++j) if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return WINO_ERR_ALIAS;
+    }
+    const bool stored = halves == 2 || act != WINO_ACT_NONE;
+    const BackwardSpace b = backward_space(M, W, K, dt, stored);
+    if (!workspace || workspace_bytes < b.total) return WINO_ERR_WORKSPACE;
+    if (!at16(workspace)) return WINO_ERR_ALIGN;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    unsigned char* base = static_cast<unsigned char*>(workspace);
+    float* sums = reinterpret_cast<float*>(base + b.dz);
+    const void* dz = dy;
+    long long lddz = lddy;
+    if (stored) {
+        Epilogue e;
+        e.bias = bias; e.extra = dy; e.ld_extra = lddy; e.out = base; e.ld_out = b.ld; e.sums = sums; e.act = act;
+        if (launch_gemm(halves == 2 ? EP_DGLU : EP_DLINEAR, false, false, Operand{w, K}, Operand{x, ldx}, GemmShape{M, N, K}, e, 1, dt, s) != hipSuccess) return WINO_ERR_HIP;
+        dz = base; lddz = b.ld;
+    } else if (dbias && launch_column_sums(dy, lddy, M, N, sums, dt, s) != hipSuccess) {
+        return WINO_ERR_HIP;
+    }
+    if (dbias && launch_sum_rows(sums, b.sum_rows, W, dbias, s) != hipSuccess) return WINO_ERR_HIP;
+    return run_products(x, ldx, w, dz, lddz, dx, lddx, dw, M, W, K, base + b.dz + b.sums, dt, s);
+}
+
+// ---- attention ------------------------------------------------------------------------------------------------------------------------
+bool attention_dims_ok(int B, int Sq, int Skv, int H, int Hkv, int D, int dt) {
+    if (B < 1 || Sq < 1 || Skv < 1 || H < 1 || Hkv < 1 || H % Hkv || D < 8 || D % 8 || D > (dt == WINO_F32 ? 160 : 256)) return false;
+    const long long most = 1LL << 30, elements = 1LL << 40;
+    return (long long)H * Sq <= most && Skv <= most && (long long)B * Hkv <= (1LL << 24) && (long long)B * H * Sq <= most && (long long)B * H * Sq * D <= elements &&
+           (long long)B * Hkv * Skv <= most && (long long)B * Hkv * Skv * D <= elements;
+}
+int tensor_status(const wino_tensor& t, size_t es, bool out, int B, int S, int H) {
+    if (!t.data) return WINO_ERR_NULL;
+    const long long st[3] = {t.stride_b, t.stride_s, t.stride_h};
+    const int n[3] = {B, S, H};
+    for (int i = 0; i < 3; ++i) {
+        if (n[i] == 1) continue;                           // a stride that is not used
+        if (st[i] < 0 || st[i] > (1LL << 36) || (out && st[i] == 0)) return WINO_ERR_DIM;
+        if (((size_t)st[i] * es) & 15u) return WINO_ERR_ALIGN;
+    }
+    return at16(t.data) ? WINO_OK : WINO_ERR_ALIGN;
+}
+size_t tensor_extent(const wino_tensor& t, size_t es, int B, int S, int H, int D) {
+    return ((size_t)(B > 1 ? (B - 1) * t.stride_b : 0) + (size_t)(S > 1 ? (S - 1) * t.stride_s : 0) + (size_t)(H > 1 ? (H - 1) * t.stride_h : 0) + (size_t)D) * es;
+}
+AttnTensor inner(const wino_tensor& t) { return AttnTensor{t.data, t.stride_b, t.stride_s, t.stride_h}; }
+
+int attention_status(const wino_attention_args* a, bool backward) {
+    if (!a) return WINO_ERR_NULL;
+    if (!is_dtype(a->dtype)) return WINO_ERR_DTYPE;
+    if (!attention_dims_ok(a->B, a->Sq, a->Skv, a->H, a->Hkv, a->D, a->dtype) || !(a->scale > 0.f) || !isfinite(a->scale)) return WINO_ERR_DIM;
+    const size_t es = bytes_of(a->dtype);
+    struct Item { const wino_tensor* t; bool out, key; };
+    const Item fwd[4] = {{&a->q, false, false}, {&a->k, false, true}, {&a->v, false, true}, {&a->o, true, false}};
+    const Item bwd[8] = {{&a->q, false, false}, {&a->k, false, true}, {&a->v, false, true}, {&a->o, false, false},
+                         {&a->d_o, false, false}, {&a->dq, true, false}, {&a->dk, true, true}, {&a->dv, true, true}};
+    const Item* items = backward ? bwd : fwd;
+    const int n = backward ? 8 : 4;
+    for (int i = 0; i < n; ++i) {
+        const int rc = tensor_status(*items[i].t, es, items[i].out, a->B, items[i].key ? a->Skv : a->Sq, items[i].key ? a->Hkv : a->H);
+        if (rc != WINO_OK) return rc;
+    }
+    if (backward && !a->lse) return WINO_ERR_NULL;
+    if (!at4(a->lse) || !at4(a->kv_len)) return WINO_ERR_ALIGN;
+    auto size = [&](const Item& x) { return tensor_extent(*x.t, es, a->B, x.key ? a->Skv : a->Sq, x.key ? a->Hkv : a->H, a->D); };
+    for (int i = 0; i < n; ++i) {
+        if (!items[i].out) continue;
+        const void* p = items[i].t->data;
+        const size_t np = size(items[i]);
+        for (int j = 0; j < n; ++j) {
+            if (j == i) continue;
+            // gradients may share a packed buffer: only the same place twice is refused there
+            if (items[j].out ? p == items[j].t->data : overlap(p, np, items[j].t->data, size(items[j]))) return WINO_ERR_ALIAS;
+        }
+        if (overlap(p, np, a->lse, (size_t)a->B * a->H * a->Sq * 4) || overlap(p, np, a->kv_len, (size_t)a->B * 4) ||
+            overlap(p, np, a->key_mask, (size_t)a->B * a->Skv))
+            return WINO_ERR_ALIAS;
+    }
+    return WINO_OK;
+}
+
+AttnArgs attention_args(const wino_attention_args* a, void* workspace) {
+    AttnArgs r{};
+    r.B = a->B; r.Sq = a->Sq; r.Skv = a->Skv; r.H = a->H; r.Hkv = a->Hkv; r.D = a->D; r.scale = a->scale;
+    r.q = inner(a->q); r.k = inner(a->k); r.v = inner(a->v); r.o = inner(a->o); r.dout = inner(a->d_o);
+    r.dq = inner(a->dq); r.dk = inner(a->dk); r.dv = inner(a->dv);
+    r.lse = a->lse; r.kv_len = a->kv_len; r.key_mask = a->key_mask;
+    r.ws = static_cast<float*>(workspace);
+    return r;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t wino_linear_workspace_bytes(int M, int N, int K, int dtype, int act) {
+    if (!is_dtype(dtype) || !is_act(act) || !product_dims_ok(M, N, K, 1)) return 0;
+    return product_bytes(M, N, K, dtype);
+}
+
+int wino_linear(const void* x, const void* w, const float* bias, const void* residual, void* y, int M, int N, int K, long long ldx, long long ldr,
+                long long ldy, int dtype, int act, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!x || !w || !y) return WINO_ERR_NULL;
+    if (!is_dtype(dtype)) return WINO_ERR_DTYPE;
+    if (!is_act(act)) return WINO_ERR_VARIANT;
+    if (!product_dims_ok(M, N, K, 1) || !ld_ok(ldx, K) || !ld_ok(ldy, N) || (residual && !ld_ok(ldr, N))) return WINO_ERR_DIM;
+    if (!at16(x) || !at16(w) || !at16(y) || !at16(residual) || !at4(bias)) return WINO_ERR_ALIGN;
+    const size_t es = bytes_of(dtype), ny = extent(M, ldy, N, es);
+    if (overlap(y, ny, x, extent(M, ldx, K, es)) || overlap(y, ny, w, (size_t)N * K * es) || overlap(y, ny, bias, (size_t)N * 4)) return WINO_ERR_ALIAS;
+    if (residual && !(residual == y && ldr == ldy) && overlap(y, ny, residual, extent(M, ldr, N, es))) return WINO_ERR_ALIAS;
+    const size_t need = product_bytes(M, N, K, dtype);
+    if (need && (!workspace || workspace_bytes < need)) return WINO_ERR_WORKSPACE;
+    if (need && !at16(workspace)) return WINO_ERR_ALIGN;
+    Epilogue e;
+    e.bias = bias; e.extra = residual; e.ld_extra = ldr; e.out = y; e.ld_out = ldy; e.act = act;
+    return product(EP_LINEAR, false, false, Operand{w, K}, Operand{x, ldx}, GemmShape{M, N, K}, e, workspace, dtype, static_cast<hipStream_t>(stream)) == hipSuccess
+               ? WINO_OK : WINO_ERR_HIP;
+}
+
+size_t wino_linear_backward_workspace_bytes(int M, int N, int K, int dtype, int act) {
+    if (!is_dtype(dtype) || !is_act(act) || !product_dims_ok(M, N, K, 1)) return 0;
+    return backward_space(M, N, K, dtype, act != WINO_ACT_NONE).total;
+}
+
+int wino_linear_backward(const void* x, const void* w, const float* bias, const void* dy, void* dx, void* dw, float* dbias, int M, int N, int K, long long ldx,
+                         long long lddy, long long lddx, int dtype, int act, void* workspace, size_t workspace_bytes, void* stream) {
+    return products_backward(x, w, bias, dy, dx, dw, dbias, M, N, K, ldx, lddy, lddx, dtype, act, 1, workspace, workspace_bytes, stream);
+}
+
+size_t wino_glu_workspace_bytes(int, int, int, int, int) { return 0; }
+
+int wino_glu(const void* x, const void* w, const float* bias, void* h, int M, int N, int K, long long ldx, long long ldh, int dtype, int act,
+             void* workspace, size_t workspace_bytes, void* stream) {
+    (void)workspace; (void)workspace_bytes;
+    if (!x || !w || !h) return WINO_ERR_NULL;
+    if (!is_dtype(dtype)) return WINO_ERR_DTYPE;
+    if (!is_act(act)) return WINO_ERR_VARIANT;
+    if (!product_dims_ok(M, N, K, 2) || !ld_ok(ldx, K) || !ld_ok(ldh, N)) return WINO_ERR_DIM;
+    if (!at16(x) || !at16(w) || !at16(h) || !at4(bias)) return WINO_ERR_ALIGN;
+    const size_t es = bytes_of(dtype), nh = extent(M, ldh, N, es);
+    if (overlap(h, nh, x, extent(M, ldx, K, es)) || overlap(h, nh, w, 2 * (size_t)N * K * es) || overlap(h, nh, bias, 2 * (size_t)N * 4)) return WINO_ERR_ALIAS;
+    Epilogue e;
+    e.bias = bias; e.out = h; e.ld_out = ldh; e.act = act;
+    return launch_gemm(EP_GLU, false, false, Operand{w, K}, Operand{x, ldx}, GemmShape{M, N, K}, e, 1, dtype, static_cast<hipStream_t>(stream)) == hipSuccess
+               ? WINO_OK : WINO_ERR_HIP;
+}
+
+size_t wino_glu_backward_workspace_bytes(int M, int N, int K, int dtype, int act) {
+    if (!is_dtype(dtype) || !is_act(act) || !product_dims_ok(M, N, K, 2)) return 0;
+    return backward_space(M, 2 * N, K, dtype, true).total;
+}
+
+int wino_glu_backward(const void* x, const void* w, const float* bias, const void* dh, void* dx, void* dw, float* dbias, int M, int N, int K, long long ldx,
+                      long long lddh, long long lddx, int dtype, int act, void* workspace, size_t workspace_bytes, void* stream) {
+    return products_backward(x, w, bias, dh, dx, dw, dbias, M, N, K, ldx, lddh, lddx, dtype, act, 2, workspace, workspace_bytes, stream);
+}
+
+size_t wino_attention_workspace_bytes(int B, int Sq, int Skv, int H, int Hkv, int D, int dtype) {
+    if (!is_dtype(dtype) || !attention_dims_ok(B, Sq, Skv, H, Hkv, D, dtype)) return 0;
+    return attention_ws_bytes(B, Sq, Skv, H, Hkv, D, dtype);
+}
+
+int wino_attention(const wino_attention_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = attention_status(a, false);
+    if (rc != WINO_OK) return rc;
+    const size_t need = attention_ws_bytes(a->B, a->Sq, a->Skv, a->H, a->Hkv, a->D, a->dtype);
+    if (need && (!workspace || workspace_bytes < need)) return WINO_ERR_WORKSPACE;
+    if (need && !at16(workspace)) return WINO_ERR_ALIGN;
+    return launch_attention(attention_args(a, workspace), a->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? WINO_OK : WINO_ERR_HIP;
+}
+
+size_t wino_attention_backward_workspace_bytes(int B, int Sq, int Skv, int H, int Hkv, int D, int dtype) {
+    if (!is_dtype(dtype) || !attention_dims_ok(B, Sq, Skv, H, Hkv, D, dtype)) return 0;
+    return attention_backward_ws_bytes(B, Sq, Skv, H, Hkv, D, dtype);
+}
+
+int wino_attention_backward(const wino_attention_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = attention_status(a, true);
+    if (rc != WINO_OK) return rc;
+    const size_t need = attention_backward_ws_bytes(a->B, a->Sq, a->Skv, a->H, a->Hkv, a->D, a->dtype);
+    if (!workspace || workspace_bytes < need) return WINO_ERR_WORKSPACE;
+    if (!at16(workspace)) return WINO_ERR_ALIGN;
+    return launch_attention_backward(attention_args(a, workspace), a->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? WINO_OK : WINO_ERR_HIP;
+}
+
+}  // extern "C"

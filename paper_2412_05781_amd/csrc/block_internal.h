@@ -1,0 +1,73 @@
+// Declarations shared by the sources of the transformer-block operators: matrix products with an epilogue (linear.hip), the gated
+// feed-forward block (the same products, two weight blocks per tile) and attention (attention.hip, attention_backward.hip).
+#pragma once
+#include "wino_internal.h"
+
+namespace wino {
+
+// Values of wino_act.
+enum { ACT_NONE = 0, ACT_SILU = 1, ACT_GELU = 2, ACT_GELU_TANH = 3 };
+
+// out[m][n] = sum_k Q(m,k) P(n,k).  An operand is stored with its reduction index contiguous, element (i,k) at p[i*ld + k], or
+// transposed, element (i,k) at p[k*ld + i].
+struct Operand {
+    const void* p;
+    long long ld;
+};
+
+// What becomes of the sums of a tile.
+enum {
+    EP_STORE = 0,      // out = sum
+    EP_LINEAR = 1,     // out = act(sum + bias) + extra                     (extra: residual, may be null)
+    EP_DLINEAR = 2,    // out = extra * act'(sum + bias)                    (extra: dy);       column sums of out to `sums`
+    EP_GLU = 3,        // out = u * act(g)                                  u, g: rows n and N + n of P
+    EP_DGLU = 4,       // out[n] = extra * act(g), out[N+n] = extra * u * act'(g)  (extra: dh); column sums of out to `sums`
+    EP_PART = 5        // fp32 sums of one range of the reduction to `part`
+};
+
+struct Epilogue {
+    const float* bias = nullptr;     // [N], EP_GLU / EP_DGLU [2N]; may be null
+    const void* extra = nullptr;     // [M][N] in the storage type
+    long long ld_extra = 0;
+    void* out = nullptr;
+    long long ld_out = 0;
+    float* sums = nullptr;           // [sum_rows][width of out]
+    float* part = nullptr;           // [nsplit][M][N]
+    int act = ACT_NONE;
+};
+
+// M rows and N columns of out (EP_GLU / EP_DGLU: N gate pairs, P has 2N rows), reduction length K.
+struct GemmShape { int M, N, K; };
+
+bool gemm_dims_ok(long long M, long long N, long long K);
+// number of rows of Epilogue::sums that a launch with EP_DLINEAR / EP_DGLU fills
+int gemm_sum_rows(int M, int dt);
+// ranges the reduction of a plain product (EP_STORE, EP_LINEAR) is cut into
+int gemm_ranges(int M, int N, int K, int dt);
+hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit,
+                       int dt, hipStream_t s);
+// out = act(sum over ranges + bias) + extra
+hipError_t launch_join(const float* part, int nsplit, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s);
+// column sums: out[c] = sum over rows of part[row][c]; and of a stored tensor, in two steps
+hipError_t launch_sum_rows(const float* part, int rows, int cols, float* out, hipStream_t s);
+int column_sum_rows(int M);
+hipError_t launch_column_sums(const void* x, long long ld, int M, int N, float* part, int dt, hipStream_t s);
+
+// One call of the attention operators; strides in elements, the last dimension contiguous.
+struct AttnTensor { const void* p; long long b, s, h; };
+struct AttnArgs {
+    int B, Sq, Skv, H, Hkv, D;
+    float scale;
+    AttnTensor q, k, v, o, dout;
+    AttnTensor dq, dk, dv;
+    float* lse;                      // [B][H][Sq], natural logarithm; may be null in the forward pass
+    const int* kv_len;               // [B] or null
+    const unsigned char* key_mask;   // [B][Skv] or null
+    float* ws;
+};
+size_t attention_ws_bytes(int B, int Sq, int Skv, int H, int Hkv, int D, int dt);
+size_t attention_backward_ws_bytes(int B, int Sq, int Skv, int H, int Hkv, int D, int dt);
+hipError_t launch_attention(const AttnArgs& a, int dt, hipStream_t s);
+hipError_t launch_attention_backward(const AttnArgs& a, int dt, hipStream_t s);
+
+}  // namespace wino

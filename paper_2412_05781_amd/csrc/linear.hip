@@ -1,0 +1,446 @@
+// Matrix products of a transformer block with what follows them in the epilogue:
+//   out[m][n] = sum_k Q(m,k) P(n,k)
+// with either operand stored along k or across it, so that one kernel serves x W^T, dz W and dz^T x.
+//
+// MFMA tiles hold n in their rows and m in their columns: a lane then owns four neighbouring n of one row m per four accumulator registers
+// and stores them together.  For the gated block a tile holds as many rows of the up weights as of the gate weights, dealt to the waves such that
+// a lane owns u and g of the same (m, n).
+#include "block_act.h"
+#include "wino_mma.h"
+
+namespace wino {
+
+namespace {
+
+// ---- LDS tiles ------------------------------------------------------------------------------------------------------------------------
+// Operand along k: rows of 128 bytes, chunk c of row r at c ^ ((r >> 1) & 7).  Operand across k: one row of BI elements per k, chunk c of row r at
+// c ^ swz(r), such that the four rows that a transposing read takes (two-byte types) or the two rows that the halves of a wave take (fp32) lie
+// in different banks.
+template <typename E, int BI> __device__ __forceinline__ int swz_across(int r) {
+    if constexpr (sizeof(E) == 4) return ((r >> 2) & 1) << 3;
+    return BI == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2;           // 64 elements: neighbouring rows lie 128 bytes apart already
+}
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+// the 16 bytes that lane `lane` gives to one 32x32 MFMA step: index i0 + lane % 32, reduction elements of step ks
+template <typename E, bool ACROSS, int BI> __device__ __forceinline__ u32x4_t read_fragment(const unsigned char* tile, int i0, int ks, int lane) {
+    const int half = lane >> 5;
+    if constexpr (!ACROSS) {
+        const int row = i0 + (lane & 31), chunk = (2 * ks + half) ^ ((row >> 1) & 7);
+        return *reinterpret_cast<const u32x4_t*>(tile + row * 128 + chunk * 16);
+    } else if constexpr (sizeof(E) == 2) {
+        // four rows k x 16 columns per 16 lanes and read; lane i of the 16 gets column i
+        const int col = i0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+        u32x4_t f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int row = 16 * ks + 8 * half + 4 * t + ((lane & 15) >> 2);
+            const unsigned char* at = tile + row * (BI * 2) + (((col >> 3) ^ swz_across<E, BI>(row)) << 4) + ((col & 4) << 1);
+            const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)at);
+            const uint2 w = __builtin_bit_cast(uint2, v);
+            f[2 * t] = w.x;
+            f[2 * t + 1] = w.y;
+        }
+        return f;
+    } else {
+        const int col = i0 + (lane & 31);
+        u32x4_t f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int row = 8 * ks + 4 * half + j;
+            f[j] = *reinterpret_cast<const uint32_t*>(tile + row * (BI * 4) + (((col >> 2) ^ swz_across<E, BI>(row)) << 4) + ((col & 3) << 2));
+        }
+        return f;
+    }
+}
+
+// n elements (up to 16 bytes) from p, the rest zero
+template <typename E> __device__ __forceinline__ u32x4_t load_part(const E* p, int n) {
+    u32x4_t f = {0, 0, 0, 0};
+    constexpr int V = 16 / (int)sizeof(E);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        if (i < n) {
+            if constexpr (sizeof(E) == 4) f[i] = *reinterpret_cast<const uint32_t*>(p + i);
+            else f[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + i) << (16 * (i & 1));
+        }
+    }
+    return f;
+}
+
+// four neighbouring elements of a row: as one access where every row allows it
+template <typename E> __device__ __forceinline__ void load4(const E* p, int n, bool whole, float* v) {
+    if (whole && n >= 4) {
+        if constexpr (sizeof(E) == 4) {
+            const float4 f = *reinterpret_cast<const float4*>(p);
+            v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+        } else {
+            const uint2 f = *reinterpret_cast<const uint2*>(p);
+            v[0] = lo16<E>(f.x); v[1] = hi16<E>(f.x); v[2] = lo16<E>(f.y); v[3] = hi16<E>(f.y);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = i < n ? to_f32<E>(p[i]) : 0.f;
+}
+template <typename E> __device__ __forceinline__ void store4(E* p, int n, bool whole, const float* v) {
+    if (whole && n >= 4) {
+        if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        else *reinterpret_cast<uint2*>(p) = make_uint2(pack2<E>(v[0], v[1]), pack2<E>(v[2], v[3]));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (i < n) p[i] = from_f32<E>(v[i]);
+}
+
+// four columns n0.. of row m, from the sums of one lane; returns in c (and c2: the gate half) what the column sums take
+template <typename E, int EP, int ACT>
+__device__ __forceinline__ void finish4(const GemmShape& g, const Epilogue& e, long long m, int n0, const float* s, const float* s2, bool whole, float* c, float* c2) {
+    const int n = g.N - n0;
+    float a[4];
+    if constexpr (EP == EP_STORE) {
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, whole, s);
+    } else if constexpr (EP == EP_LINEAR) {
+        float r[4] = {0.f, 0.f, 0.f, 0.f};
+        if (e.extra) load4<E>(static_cast<const E*>(e.extra) + m * e.ld_extra + n0, n, whole, r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float b = e.bias && i < n ? e.bias[n0 + i] : 0.f;
+            a[i] = act_only<E, ACT>(s[i] + b) + r[i];
+        }
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, whole, a);
+    } else if constexpr (EP == EP_DLINEAR) {
+        float r[4];
+        load4<E>(static_cast<const E*>(e.extra) + m * e.ld_extra + n0, n, whole, r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float b = e.bias && i < n ? e.bias[n0 + i] : 0.f;
+            float v, d;
+            act_both<E, ACT>(s[i] + b, v, d);
+            c[i] = i < n ? r[i] * d : 0.f;
+        }
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, whole, c);
+    } else if constexpr (EP == EP_GLU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float bu = e.bias && i < n ? e.bias[n0 + i] : 0.f, bg = e.bias && i < n ? e.bias[g.N + n0 + i] : 0.f;
+            a[i] = (s[i] + bu) * act_only<E, ACT>(s2[i] + bg);
+        }
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, whole, a);
+    } else if constexpr (EP == EP_DGLU) {
+        float r[4];
+        load4<E>(static_cast<const E*>(e.extra) + m * e.ld_extra + n0, n, whole, r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float bu = e.bias && i < n ? e.bias[n0 + i] : 0.f, bg = e.bias && i < n ? e.bias[g.N + n0 + i] : 0.f;
+            float v, d;
+            act_both<E, ACT>(s2[i] + bg, v, d);
+            c[i] = i < n ? r[i] * v : 0.f;
+            c2[i] = i < n ? r[i] * (s[i] + bu) * d : 0.f;
+        }
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, whole, c);
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + g.N + n0, n, whole, c2);
+    }
+}
+
+// whether rows of four neighbouring elements can be read and written as one access
+template <typename E> __device__ __forceinline__ bool rows_whole(const GemmShape& g, const Epilogue& e) {
+    constexpr int A = 4 * (int)sizeof(E);
+    uintptr_t bits = reinterpret_cast<uintptr_t>(e.out) | (uintptr_t)(e.ld_out * (long long)sizeof(E)) | (uintptr_t)(g.N * (int)sizeof(E));
+    if (e.extra) bits |= reinterpret_cast<uintptr_t>(e.extra) | (uintptr_t)(e.ld_extra * (long long)sizeof(E));
+    return (bits & (A - 1)) == 0;
+}
+
+__device__ __forceinline__ float sum_over_32(float v) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+// ---- the kernel for every shape: operands go through registers, element by element where alignment or the edge asks for it -------------------
+constexpr int kBP = 128, kBQ = 64;       // tile: 128 rows of P x 64 rows of Q, four waves, 64 x 32 each
+
+template <typename E, int EP, int ACT, bool PA, bool QA>
+__global__ void __launch_bounds__(256) gemm_any_kernel(Operand P, Operand Q, GemmShape g, Epilogue e, int tiles_p, int tiles_q, int total, int per_xcd,
+                                                       int nsplit, bool p_vec, bool q_vec) {
+    constexpr bool GLU = EP == EP_GLU || EP == EP_DGLU;
+    constexpr int BK = 128 / (int)sizeof(E), V = 16 / (int)sizeof(E);
+    constexpr int P_CHUNKS = kBP * 8 / 256, Q_CHUNKS = kBQ * 8 / 256;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[(kBP + kBQ) * 128];
+    unsigned char* tp = lds;
+    unsigned char* tq = lds + kBP * 128;
+
+    const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+    if (logical >= total) return;                          // uniform per workgroup, before any barrier
+    const int split = logical / (tiles_p * tiles_q), in = logical - split * (tiles_p * tiles_q);
+    const int bq = in / tiles_p, bp = in - bq * tiles_p;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wp = wave & 1, wq = wave >> 1;
+    constexpr int BN = GLU ? kBP / 2 : kBP;                // columns of out per tile
+    const int n0 = bp * BN;
+    const long long m0 = (long long)bq * kBQ;
+    const int nk = (g.K + BK - 1) / BK;
+    const int k_begin = (int)((long long)split * nk / nsplit), k_end = (int)((long long)(split + 1) * nk / nsplit);
+
+    const E* pp = static_cast<const E*>(P.p);
+    const E* qp = static_cast<const E*>(Q.p);
+    // row r of the P tile is row p_row(r) of P, if r stands for an n inside the matrix
+    auto p_row = [&](int r) { return GLU && r >= kBP / 2 ? g.N + n0 + r - kBP / 2 : n0 + r; };
+    auto p_left = [&](int r) { const int n = n0 + (GLU && r >= kBP / 2 ? r - kBP / 2 : r); return g.N - n; };      // <= 0: outside
+    u32x4_t rp[P_CHUNKS], rq[Q_CHUNKS];
+    const u32x4_t zero = {0, 0, 0, 0};
+    auto fetch = [&](int kt) {
+        const int k0 = kt * BK;
+#pragma unroll
+        for (int i = 0; i < P_CHUNKS; ++i) {
+            const int id = tid + 256 * i;
+            if constexpr (!PA) {
+                const int r = id >> 3, k = k0 + (id & 7) * V, n = p_left(r) > 0 ? g.K - k : 0;
+                const E* at = pp + (long long)p_row(r) * P.ld + k;
+                rp[i] = n <= 0 ? zero : p_vec && n >= V ? *reinterpret_cast<const u32x4_t*>(at) : load_part<E>(at, n);
+            } else {
+                constexpr int CPR = kBP / V;
+                const int k = k0 + id / CPR, r = (id % CPR) * V, n = k < g.K ? p_left(r) : 0;
+                const E* at = pp + (long long)k * P.ld + p_row(r);
+                rp[i] = n <= 0 ? zero : p_vec && n >= V ? *reinterpret_cast<const u32x4_t*>(at) : load_part<E>(at, n);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < Q_CHUNKS; ++i) {
+            const int id = tid + 256 * i;
+            if constexpr (!QA) {
+                const int k = k0 + (id & 7) * V;
+                const long long m = m0 + (id >> 3);
+                const int n = m < g.M ? g.K - k : 0;
+                const E* at = qp + m * Q.ld + k;
+                rq[i] = n <= 0 ? zero : q_vec && n >= V ? *reinterpret_cast<const u32x4_t*>(at) : load_part<E>(at, n);
+            } else {
+                constexpr int CPR = kBQ / V;
+                const int k = k0 + id / CPR;
+                const long long m = m0 + (id % CPR) * V;
+                const long long left = k < g.K ? g.M - m : 0;
+                const int n = left > V ? V : (int)left;
+                const E* at = qp + (long long)k * Q.ld + m;
+                rq[i] = n <= 0 ? zero : q_vec && n >= V ? *reinterpret_cast<const u32x4_t*>(at) : load_part<E>(at, n);
+            }
+        }
+    };
+    auto put = [&]() {
+#pragma unroll
+        for (int i = 0; i < P_CHUNKS; ++i) {
+            const int id = tid + 256 * i;
+            if constexpr (!PA) { const int r = id >> 3; *reinterpret_cast<u32x4_t*>(tp + r * 128 + (((id & 7) ^ ((r >> 1) & 7)) << 4)) = rp[i]; }
+            else { constexpr int CPR = kBP / V; const int r = id / CPR; *reinterpret_cast<u32x4_t*>(tp + r * (kBP * (int)sizeof(E)) + (((id % CPR) ^ swz_across<E, kBP>(r)) << 4)) = rp[i]; }
+        }
+#pragma unroll
+        for (int i = 0; i < Q_CHUNKS; ++i) {
+            const int id = tid + 256 * i;
+            if constexpr (!QA) { const int r = id >> 3; *reinterpret_cast<u32x4_t*>(tq + r * 128 + (((id & 7) ^ ((r >> 1) & 7)) << 4)) = rq[i]; }
+            else {
+                constexpr int CPR = kBQ / V;
+                const int r = id / CPR;
+                *reinterpret_cast<u32x4_t*>(tq + r * (kBQ * (int)sizeof(E)) + (((id % CPR) ^ swz_across<E, kBQ>(r)) << 4)) = rq[i];
+            }
+        }
+    };
+
+    float16_t acc[2] = {};
+    if (k_begin < k_end) fetch(k_begin);
+    for (int kt = k_begin; kt < k_end; ++kt) {
+        __syncthreads();                                   // the tile has been read
+        put();
+        __syncthreads();
+        if (kt + 1 < k_end) fetch(kt + 1);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            const u32x4_t fq = read_fragment<E, QA, kBQ>(tq, wq * 32, ks, lane);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) Mma<E>::run(read_fragment<E, PA, kBP>(tp, i * 64 + wp * 32, ks, lane), fq, acc[i]);
+        }
+    }
+
+    // register r of lane l holds row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32 of a 32x32 tile
+    const long long m = m0 + wq * 32 + (lane & 31);
+    const int half = lane >> 5;
+    if constexpr (EP == EP_PART) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int n = n0 + i * 64 + wp * 32 + 8 * (r / 4) + 4 * half + r % 4;
+                if (m < g.M && n < g.N) e.part[((long long)split * g.M + m) * g.N + n] = acc[i][r];
+            }
+        return;
+    }
+    const bool whole = rows_whole<E>(g, e);
+    constexpr bool SUMS = EP == EP_DLINEAR || EP == EP_DGLU;
+#pragma unroll
+    for (int i = 0; i < (GLU ? 1 : 2); ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int n = n0 + i * 64 + wp * 32 + 8 * q + 4 * half;
+            float s[4], s2[4], c[4] = {}, c2[4] = {};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { s[j] = acc[i][4 * q + j]; s2[j] = acc[1][4 * q + j]; }
+            if (m < g.M && n < g.N) finish4<E, EP, ACT>(g, e, m, n, s, s2, whole, c, c2);
+            if constexpr (SUMS) {
+                const long long row = (long long)bq * 2 + wq;
+                const int width = EP == EP_DGLU ? 2 * g.N : g.N;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float t = sum_over_32(c[j]);
+                    if ((lane & 31) == 0 && n + j < g.N) e.sums[row * width + n + j] = t;
+                    if constexpr (EP == EP_DGLU) {
+                        const float t2 = sum_over_32(c2[j]);
+                        if ((lane & 31) == 0 && n + j < g.N) e.sums[row * width + g.N + n + j] = t2;
+                    }
+                }
+            }
+        }
+}
+
+template <typename E> bool vec_rows(const Operand& o) {
+    return ((reinterpret_cast<uintptr_t>(o.p) | (uintptr_t)(o.ld * (long long)sizeof(E))) & 15u) == 0;
+}
+
+template <typename E, int EP, int ACT, bool PA, bool QA>
+hipError_t launch_any(const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s) {
+    constexpr bool GLU = EP == EP_GLU || EP == EP_DGLU;
+    const int bn = GLU ? kBP / 2 : kBP;
+    const long long tp = (g.N + bn - 1) / bn, tq = ((long long)g.M + kBQ - 1) / kBQ, total = tp * tq * nsplit;
+    if (total > 0x3fffffffLL) return hipErrorInvalidValue;
+    const int per_xcd = (int)((total + 7) / 8);
+    // the gate half of a transposed P starts at column N
+    const bool p_vec = vec_rows<E>(P) && !(GLU && PA && (g.N * sizeof(E)) % 16 != 0);
+    hipLaunchKernelGGL((gemm_any_kernel<E, EP, ACT, PA, QA>), dim3((unsigned)(per_xcd * 8)), dim3(256), 0, s, P, Q, g, e, (int)tp, (int)tq, (int)total, per_xcd,
+                       nsplit, p_vec, vec_rows<E>(Q));
+    return hipGetLastError();
+}
+
+template <typename E, int EP> hipError_t with_act(const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, hipStream_t s) {
+    switch (e.act) {
+        case ACT_NONE: return launch_any<E, EP, ACT_NONE, false, false>(P, Q, g, e, 1, s);
+        case ACT_SILU: return launch_any<E, EP, ACT_SILU, false, false>(P, Q, g, e, 1, s);
+        case ACT_GELU: return launch_any<E, EP, ACT_GELU, false, false>(P, Q, g, e, 1, s);
+        case ACT_GELU_TANH: return launch_any<E, EP, ACT_GELU_TANH, false, false>(P, Q, g, e, 1, s);
+        default: return hipErrorInvalidValue;
+    }
+}
+
+template <typename E, int EP> hipError_t with_layout(bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s) {
+    if (!pa && !qa) return launch_any<E, EP, ACT_NONE, false, false>(P, Q, g, e, nsplit, s);
+    if (pa && !qa) return launch_any<E, EP, ACT_NONE, true, false>(P, Q, g, e, nsplit, s);
+    if (pa && qa) return launch_any<E, EP, ACT_NONE, true, true>(P, Q, g, e, nsplit, s);
+    return hipErrorInvalidValue;
+}
+
+// ---- joining ranges, column sums ------------------------------------------------------------------------------------------------------
+template <typename E, int ACT> __global__ void __launch_bounds__(256) join_kernel(const float* part, int nsplit, GemmShape g, Epilogue e, bool linear) {
+    const long long quads = (g.N + 3) / 4, id = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (id >= quads * g.M) return;
+    const long long m = id / quads;
+    const int n0 = (int)(id - m * quads) * 4;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    const size_t step = (size_t)g.M * g.N;
+    for (int r = 0; r < nsplit; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n0 + i < g.N) s[i] += part[(size_t)r * step + (size_t)m * g.N + n0 + i];
+    const bool whole = rows_whole<E>(g, e);
+    if (linear) finish4<E, EP_LINEAR, ACT>(g, e, m, n0, s, s, whole, nullptr, nullptr);
+    else finish4<E, EP_STORE, ACT>(g, e, m, n0, s, s, whole, nullptr, nullptr);
+}
+
+__global__ void __launch_bounds__(256) sum_rows_kernel(const float* part, int rows, int cols, float* out) {
+    const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
+    __shared__ float t[4][64];
+    float a = 0.f;
+    if (c < cols)
+        for (int r = w; r < rows; r += 4) a += part[(size_t)r * cols + c];
+    t[w][threadIdx.x & 63] = a;
+    __syncthreads();
+    if (w == 0 && c < cols) out[c] = (t[0][threadIdx.x] + t[1][threadIdx.x]) + (t[2][threadIdx.x] + t[3][threadIdx.x]);
+}
+
+// 64 columns x a range of rows per workgroup
+template <typename E> __global__ void __launch_bounds__(256) column_sums_kernel(const E* x, long long ld, int M, int N, float* part) {
+    const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
+    const long long r0 = (long long)blockIdx.y * M / gridDim.y, r1 = (long long)(blockIdx.y + 1) * M / gridDim.y;
+    __shared__ float t[4][64];
+    float a = 0.f;
+    if (c < N)
+        for (long long r = r0 + w; r < r1; r += 4) a += to_f32<E>(x[r * ld + c]);
+    t[w][threadIdx.x & 63] = a;
+    __syncthreads();
+    if (w == 0 && c < N) part[(size_t)blockIdx.y * N + c] = (t[0][threadIdx.x] + t[1][threadIdx.x]) + (t[2][threadIdx.x] + t[3][threadIdx.x]);
+}
+
+}  // namespace
+
+bool gemm_dims_ok(long long M, long long N, long long K) {
+    const long long most = 1LL << 30, elements = 1LL << 40;
+    return M >= 1 && N >= 1 && K >= 1 && M <= most && N <= most / 4 && K <= most / 4 && M * N <= elements && M * K <= elements && N * K <= elements &&
+           ((M + kBQ - 1) / kBQ) * ((N + kBP / 2 - 1) / (kBP / 2)) <= (1LL << 26);
+}
+
+int gemm_sum_rows(int M, int) { return (int)(((long long)M + kBQ - 1) / kBQ) * 2; }
+
+// A reduction is cut where there are fewer tiles than compute units, down to ranges of 256 bytes a row.
+int gemm_ranges(int M, int N, int K, int dt) {
+    const long long tiles = (long long)((N + kBP - 1) / kBP) * ((M + kBQ - 1) / kBQ);
+    const int stages = (K + (dt == DT_F32 ? 32 : 64) - 1) / (dt == DT_F32 ? 32 : 64);
+    long long n = 512 / tiles;
+    if (n > stages / 2) n = stages / 2;
+    if (n > 16) n = 16;
+    return n < 2 ? 1 : (int)n;
+}
+
+hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, int dt, hipStream_t s) {
+    return with_dtype(dt, [&](auto* tag) -> hipError_t {
+        using E = std::remove_pointer_t<decltype(tag)>;
+        switch (ep) {
+            case EP_STORE: return with_layout<E, EP_STORE>(p_trans, q_trans, P, Q, g, e, 1, s);
+            case EP_PART: return with_layout<E, EP_PART>(p_trans, q_trans, P, Q, g, e, nsplit, s);
+            case EP_LINEAR: return with_act<E, EP_LINEAR>(P, Q, g, e, s);
+            case EP_DLINEAR: return with_act<E, EP_DLINEAR>(P, Q, g, e, s);
+            case EP_GLU: return with_act<E, EP_GLU>(P, Q, g, e, s);
+            case EP_DGLU: return with_act<E, EP_DGLU>(P, Q, g, e, s);
+            default: return hipErrorInvalidValue;
+        }
+    });
+}
+
+hipError_t launch_join(const float* part, int nsplit, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s) {
+    const long long blocks = ((long long)((g.N + 3) / 4) * g.M + 255) / 256;
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    return with_dtype(dt, [&](auto* tag) -> hipError_t {
+        using E = std::remove_pointer_t<decltype(tag)>;
+        const bool linear = e.bias || e.extra || e.act != ACT_NONE;
+        const dim3 grid((unsigned)blocks);
+        switch (e.act) {
+            case ACT_NONE: hipLaunchKernelGGL((join_kernel<E, ACT_NONE>), grid, dim3(256), 0, s, part, nsplit, g, e, linear); break;
+            case ACT_SILU: hipLaunchKernelGGL((join_kernel<E, ACT_SILU>), grid, dim3(256), 0, s, part, nsplit, g, e, linear); break;
+            case ACT_GELU: hipLaunchKernelGGL((join_kernel<E, ACT_GELU>), grid, dim3(256), 0, s, part, nsplit, g, e, linear); break;
+            default: hipLaunchKernelGGL((join_kernel<E, ACT_GELU_TANH>), grid, dim3(256), 0, s, part, nsplit, g, e, linear); break;
+        }
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_sum_rows(const float* part, int rows, int cols, float* out, hipStream_t s) {
+    hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(256), 0, s, part, rows, cols, out);
+    return hipGetLastError();
+}
+
+int column_sum_rows(int M) { return M < 64 ? 1 : M < 64 * 128 ? M / 64 : 128; }
+
+hipError_t launch_column_sums(const void* x, long long ld, int M, int N, float* part, int dt, hipStream_t s) {
+    return with_dtype(dt, [&](auto* tag) -> hipError_t {
+        using E = std::remove_pointer_t<decltype(tag)>;
+        hipLaunchKernelGGL((column_sums_kernel<E>), dim3((unsigned)((N + 63) / 64), (unsigned)column_sum_rows(M)), dim3(256), 0, s, (const E*)x, ld, M, N, part);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace wino
