@@ -43,7 +43,7 @@ BackwardSpace backward_space(int M, int W, int K, int dt, bool stored) {
     BackwardSpace b;
     b.ld = ((long long)W + 7) / 8 * 8;
     b.dz = stored ? up256((size_t)M * b.ld * bytes_of(dt)) : 0;
-    b.sum_rows = stored ? gemm_sum_rows(M, dt) : column_sum_rows(M);
+    b.sum_rows = stored ? gemm_most_sum_rows(M) : column_sum_rows(M);
     b.sums = up256((size_t)b.sum_rows * W * sizeof(float));
     const size_t px = product_bytes(M, K, W, dt), pw = product_bytes(W, K, M, dt);
     b.parts = px > pw ? px : pw;
@@ -88,7 +88,7 @@ int products_backward(const void* x, const void* w, const float* bias, const voi
         for (int j = 0; j < i; ++j) if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return WINO_ERR_ALIAS;
     }
     const bool stored = halves == 2 || act != WINO_ACT_NONE;
-    const BackwardSpace b = backward_space(M, W, K, dt, stored);
+    BackwardSpace b = backward_space(M, W, K, dt, stored);
     if (!workspace || workspace_bytes < b.total) return WINO_ERR_WORKSPACE;
     if (!at16(workspace)) return WINO_ERR_ALIGN;
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -99,7 +99,7 @@ int products_backward(const void* x, const void* w, const float* bias, const voi
     if (stored) {
         Epilogue e;
         e.bias = bias; e.extra = dy; e.ld_extra = lddy; e.out = base; e.ld_out = b.ld; e.sums = sums; e.act = act;
-        if (launch_gemm(halves == 2 ? EP_DGLU : EP_DLINEAR, false, false, Operand{w, K}, Operand{x, ldx}, GemmShape{M, N, K}, e, 1, dt, s) != hipSuccess) return WINO_ERR_HIP;
+        if (launch_gemm(halves == 2 ? EP_DGLU : EP_DLINEAR, false, false, Operand{w, K}, Operand{x, ldx}, GemmShape{M, N, K}, e, 1, dt, s, &b.sum_rows) != hipSuccess) return WINO_ERR_HIP;
         dz = base; lddz = b.ld;
     } else if (dbias && launch_column_sums(dy, lddy, M, N, sums, dt, s) != hipSuccess) {
         return WINO_ERR_HIP;

@@ -40,12 +40,12 @@ struct Epilogue {
 struct GemmShape { int M, N, K; };
 
 bool gemm_dims_ok(long long M, long long N, long long K);
-// number of rows of Epilogue::sums that a launch with EP_DLINEAR / EP_DGLU fills
-int gemm_sum_rows(int M, int dt);
+// rows of Epilogue::sums that a launch with EP_DLINEAR / EP_DGLU may fill; launch_gemm says how many it did (sum_rows, may be null)
+int gemm_most_sum_rows(int M);
 // ranges the reduction of a plain product (EP_STORE, EP_LINEAR) is cut into
 int gemm_ranges(int M, int N, int K, int dt);
 hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit,
-                       int dt, hipStream_t s);
+                       int dt, hipStream_t s, int* sum_rows = nullptr);
 // out = act(sum over ranges + bias) + extra
 hipError_t launch_join(const float* part, int nsplit, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s);
 // column sums: out[c] = sum over rows of part[row][c]; and of a stored tensor, in two steps

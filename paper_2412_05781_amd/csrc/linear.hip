@@ -5,95 +5,11 @@
 // MFMA tiles hold n in their rows and m in their columns: a lane then owns four neighbouring n of one row m per four accumulator registers
 // and stores them together.  For the gated block a tile holds as many rows of the up weights as of the gate weights, dealt to the waves such that
 // a lane owns u and g of the same (m, n).
-#include "block_act.h"
-#include "wino_mma.h"
+#include "linear_tile.h"
 
 namespace wino {
 
 namespace {
-
-// ---- LDS tiles ------------------------------------------------------------------------------------------------------------------------
-// Operand along k: rows of 128 bytes, chunk c of row r at c ^ ((r >> 1) & 7).  Operand across k: one row of BI elements per k, chunk c of row r at
-// c ^ swz(r), such that the four rows that a transposing read takes (two-byte types) or the two rows that the halves of a wave take (fp32) lie
-// in different banks.
-template <typename E, int BI> __device__ __forceinline__ int swz_across(int r) {
-    if constexpr (sizeof(E) == 4) return ((r >> 2) & 1) << 3;
-    return BI == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2;           // 64 elements: neighbouring rows lie 128 bytes apart already
-}
-
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
-
-// the 16 bytes that lane `lane` gives to one 32x32 MFMA step: index i0 + lane % 32, reduction elements of step ks
-template <typename E, bool ACROSS, int BI> __device__ __forceinline__ u32x4_t read_fragment(const unsigned char* tile, int i0, int ks, int lane) {
-    const int half = lane >> 5;
-    if constexpr (!ACROSS) {
-        const int row = i0 + (lane & 31), chunk = (2 * ks + half) ^ ((row >> 1) & 7);
-        return *reinterpret_cast<const u32x4_t*>(tile + row * 128 + chunk * 16);
-    } else if constexpr (sizeof(E) == 2) {
-        // four rows k x 16 columns per 16 lanes and read; lane i of the 16 gets column i
-        const int col = i0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-        u32x4_t f;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int row = 16 * ks + 8 * half + 4 * t + ((lane & 15) >> 2);
-            const unsigned char* at = tile + row * (BI * 2) + (((col >> 3) ^ swz_across<E, BI>(row)) << 4) + ((col & 4) << 1);
-            const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)at);
-            const uint2 w = __builtin_bit_cast(uint2, v);
-            f[2 * t] = w.x;
-            f[2 * t + 1] = w.y;
-        }
-        return f;
-    } else {
-        const int col = i0 + (lane & 31);
-        u32x4_t f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int row = 8 * ks + 4 * half + j;
-            f[j] = *reinterpret_cast<const uint32_t*>(tile + row * (BI * 4) + (((col >> 2) ^ swz_across<E, BI>(row)) << 4) + ((col & 3) << 2));
-        }
-        return f;
-    }
-}
-
-// n elements (up to 16 bytes) from p, the rest zero
-template <typename E> __device__ __forceinline__ u32x4_t load_part(const E* p, int n) {
-    u32x4_t f = {0, 0, 0, 0};
-    constexpr int V = 16 / (int)sizeof(E);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        if (i < n) {
-            if constexpr (sizeof(E) == 4) f[i] = *reinterpret_cast<const uint32_t*>(p + i);
-            else f[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + i) << (16 * (i & 1));
-        }
-    }
-    return f;
-}
-
-// four neighbouring elements of a row: as one access where every row allows it
-template <typename E> __device__ __forceinline__ void load4(const E* p, int n, bool whole, float* v) {
-    if (whole && n >= 4) {
-        if constexpr (sizeof(E) == 4) {
-            const float4 f = *reinterpret_cast<const float4*>(p);
-            v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
-        } else {
-            const uint2 f = *reinterpret_cast<const uint2*>(p);
-            v[0] = lo16<E>(f.x); v[1] = hi16<E>(f.x); v[2] = lo16<E>(f.y); v[3] = hi16<E>(f.y);
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = i < n ? to_f32<E>(p[i]) : 0.f;
-}
-template <typename E> __device__ __forceinline__ void store4(E* p, int n, bool whole, const float* v) {
-    if (whole && n >= 4) {
-        if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-        else *reinterpret_cast<uint2*>(p) = make_uint2(pack2<E>(v[0], v[1]), pack2<E>(v[2], v[3]));
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) if (i < n) p[i] = from_f32<E>(v[i]);
-}
 
 // four columns n0.. of row m, from the sums of one lane; returns in c (and c2: the gate half) what the column sums take
 template <typename E, int EP, int ACT>
@@ -300,10 +216,6 @@ __global__ void __launch_bounds__(256) gemm_any_kernel(Operand P, Operand Q, Gem
         }
 }
 
-template <typename E> bool vec_rows(const Operand& o) {
-    return ((reinterpret_cast<uintptr_t>(o.p) | (uintptr_t)(o.ld * (long long)sizeof(E))) & 15u) == 0;
-}
-
 template <typename E, int EP, int ACT, bool PA, bool QA>
 hipError_t launch_any(const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s) {
     constexpr bool GLU = EP == EP_GLU || EP == EP_DGLU;
@@ -384,7 +296,8 @@ bool gemm_dims_ok(long long M, long long N, long long K) {
            ((M + kBQ - 1) / kBQ) * ((N + kBP / 2 - 1) / (kBP / 2)) <= (1LL << 26);
 }
 
-int gemm_sum_rows(int M, int) { return (int)(((long long)M + kBQ - 1) / kBQ) * 2; }
+// workgroups of 64 rows with two waves across them, of 128 with two or of 256 with four
+int gemm_most_sum_rows(int M) { return (M + 63) / 64 * 2 + 4; }
 
 // A reduction is cut where there are fewer tiles than compute units, down to ranges of 256 bytes a row.
 int gemm_ranges(int M, int N, int K, int dt) {
@@ -396,7 +309,10 @@ int gemm_ranges(int M, int N, int K, int dt) {
     return n < 2 ? 1 : (int)n;
 }
 
-hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, int dt, hipStream_t s) {
+hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, int dt, hipStream_t s,
+                       int* sum_rows) {
+    if (tile_gemm_ok(ep, p_trans, q_trans, P, Q, g, e, dt)) return launch_tile_gemm(ep, p_trans, q_trans, P, Q, g, e, nsplit, dt, s, sum_rows);
+    if (sum_rows) *sum_rows = (g.M + kBQ - 1) / kBQ * 2;
     return with_dtype(dt, [&](auto* tag) -> hipError_t {
         using E = std::remove_pointer_t<decltype(tag)>;
         switch (ep) {
