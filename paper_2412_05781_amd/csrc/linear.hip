@@ -264,15 +264,22 @@ template <typename E, int ACT> __global__ void __launch_bounds__(256) join_kerne
     else finish4<E, EP_STORE, ACT>(g, e, m, n0, s, s, whole, nullptr, nullptr);
 }
 
-__global__ void __launch_bounds__(256) sum_rows_kernel(const float* part, int rows, int cols, float* out) {
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
-    __shared__ float t[4][64];
+// 64 columns per workgroup, sixteen waves that take every sixteenth row
+__global__ void __launch_bounds__(1024) sum_rows_kernel(const float* part, int rows, int cols, float* out) {
+    const int l = threadIdx.x & 63, c = blockIdx.x * 64 + l, w = threadIdx.x >> 6;
+    __shared__ float t[16][64];
     float a = 0.f;
     if (c < cols)
-        for (int r = w; r < rows; r += 4) a += part[(size_t)r * cols + c];
-    t[w][threadIdx.x & 63] = a;
+#pragma unroll 4
+        for (int r = w; r < rows; r += 16) a += part[(size_t)r * cols + c];
+    t[w][l] = a;
     __syncthreads();
-    if (w == 0 && c < cols) out[c] = (t[0][threadIdx.x] + t[1][threadIdx.x]) + (t[2][threadIdx.x] + t[3][threadIdx.x]);
+    if (w == 0 && c < cols) {
+        float v = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v += t[i][l];
+        out[c] = v;
+    }
 }
 
 // 64 columns x a range of rows per workgroup
@@ -299,12 +306,16 @@ bool gemm_dims_ok(long long M, long long N, long long K) {
 // workgroups of 64 rows with two waves across them, of 128 with two or of 256 with four
 int gemm_most_sum_rows(int M) { return (M + 63) / 64 * 2 + 4; }
 
-// A reduction is cut where there are fewer tiles than compute units, down to ranges of 256 bytes a row.
+// A reduction is cut where there are fewer tiles than compute units, into ranges long enough to be worth the join (two-byte types: sixteen stages,
+// about 5 us; fp32, whose stages last four times as long: four).
 int gemm_ranges(int M, int N, int K, int dt) {
-    const long long tiles = (long long)((N + kBP - 1) / kBP) * ((M + kBQ - 1) / kBQ);
-    const int stages = (K + (dt == DT_F32 ? 32 : 64) - 1) / (dt == DT_F32 ? 32 : 64);
-    long long n = 512 / tiles;
-    if (n > stages / 2) n = stages / 2;
+    auto tiles = [&](int n, int m) { return (((long long)N + n - 1) / n) * (((long long)M + m - 1) / m); };
+    const bool f32 = dt == DT_F32;
+    const int stages = K / (f32 ? 32 : 64);
+    if (!f32 && tiles(128, 128) >= 130) return 1;
+    long long n = f32 ? 512 / tiles(kBP, kBQ) : 768 / tiles(64, 64);
+    const int most = stages / (f32 ? 4 : 16);
+    if (n > most) n = most;
     if (n > 16) n = 16;
     return n < 2 ? 1 : (int)n;
 }
@@ -345,7 +356,7 @@ hipError_t launch_join(const float* part, int nsplit, const GemmShape& g, const 
 }
 
 hipError_t launch_sum_rows(const float* part, int rows, int cols, float* out, hipStream_t s) {
-    hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(256), 0, s, part, rows, cols, out);
+    hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, s, part, rows, cols, out);
     return hipGetLastError();
 }
 

@@ -28,8 +28,7 @@ __device__ __forceinline__ float sum_over_16(float v) {
 }
 
 // eight neighbouring elements of a row
-template <typename E> __device__ __forceinline__ void load8(const E* p, float* v) {
-    const uint4 f = *reinterpret_cast<const uint4*>(p);
+template <typename E> __device__ __forceinline__ void unpack8(const uint4& f, float* v) {
     v[0] = lo16<E>(f.x); v[1] = hi16<E>(f.x); v[2] = lo16<E>(f.y); v[3] = hi16<E>(f.y);
     v[4] = lo16<E>(f.z); v[5] = hi16<E>(f.z); v[6] = lo16<E>(f.w); v[7] = hi16<E>(f.w);
 }
@@ -38,6 +37,7 @@ template <typename E> __device__ __forceinline__ void store8(E* p, const float* 
 }
 
 // Epilogue of one wave's tile.  acc[i][j]: rows n of 32-row block i (GLU: block i of the up rows, FP / 2 + i of the gate rows), columns m of block j.
+// What a block reads besides its sums is requested for all of its columns before the first is used, from clamped places; only stores are guarded.
 template <typename E, int EP, int ACT, int FP, int FQ, int WP, int WQ>
 __device__ __forceinline__ void finish_tile(const GemmShape& g, const Epilogue& e, float16_t (&acc)[FP][FQ], int n0, long long m0, int wp, int wq, long long sum_row, int lane, int split) {
     constexpr bool GLU = EP == EP_GLU || EP == EP_DGLU, SUMS = EP == EP_DLINEAR || EP == EP_DGLU;
@@ -45,27 +45,44 @@ __device__ __forceinline__ void finish_tile(const GemmShape& g, const Epilogue& 
     const int half = lane >> 5;
     E* out = static_cast<E*>(e.out);
     const E* extra = static_cast<const E*>(e.extra);
+    const bool has_bias = EP != EP_STORE && EP != EP_PART && e.bias, has_extra = SUMS || (EP == EP_LINEAR && extra);
+    long long mrow[FQ];
+    bool m_on[FQ];
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+    for (int j = 0; j < FQ; ++j) {
+        const long long m = m0 + (j * WQ + wq) * 32 + (lane & 31);
+        m_on[j] = m < g.M;
+        mrow[j] = m_on[j] ? m : g.M - 1;
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        int n[2];
+        bool n_on[2];
+        float bias[2][8] = {}, bias2[2][8] = {};
+        uint4 ex[2][FQ] = {};
 #pragma unroll
         for (int qp = 0; qp < 2; ++qp) {
-            // after the exchange of halves a lane holds n .. n + 7 of its row
-            const int n = n0 + (i * WP + wp) * 32 + 16 * qp + 8 * half;
-            const bool n_on = n < g.N;                     // N is a multiple of 8 here
-            float bias[8] = {}, bias2[8] = {}, sum[8] = {}, sum2[8] = {};
-            if constexpr (EP != EP_STORE && EP != EP_PART) {
-                if (e.bias && n_on) {
+            // after the exchange of halves a lane holds n .. n + 7 of its row; N is a multiple of 8 here
+            const int c = n0 + (i * WP + wp) * 32 + 16 * qp + 8 * half;
+            n_on[qp] = c < g.N;
+            n[qp] = n_on[qp] ? c : g.N - 8;
+            if (has_bias) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) bias[k] = e.bias[n + k];
-                    if constexpr (GLU) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) bias2[k] = e.bias[g.N + n + k];
-                    }
+                for (int k = 0; k < 8; ++k) {
+                    bias[qp][k] = e.bias[n[qp] + k];
+                    if constexpr (GLU) bias2[qp][k] = e.bias[g.N + n[qp] + k];
                 }
             }
+            if (has_extra) {
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) ex[qp][j] = *reinterpret_cast<const uint4*>(extra + mrow[j] * e.ld_extra + n[qp]);
+            }
+        }
+#pragma unroll
+        for (int qp = 0; qp < 2; ++qp) {
+            float sum[8] = {}, sum2[8] = {};
 #pragma unroll
             for (int j = 0; j < FQ; ++j) {
-                const long long m = m0 + (j * WQ + wq) * 32 + (lane & 31);
                 float s[8], s2[8], a[8], b[8];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
@@ -78,42 +95,40 @@ __device__ __forceinline__ void finish_tile(const GemmShape& g, const Epilogue& 
                         swap_halves(s2[k], s2[k + 4]);
                     }
                 }
-                if (!(n_on && m < g.M)) continue;
+                const bool on = n_on[qp] && m_on[j];
                 if constexpr (EP == EP_PART) {
-                    float* p = e.part + ((long long)split * g.M + m) * g.N + n;
-                    *reinterpret_cast<float4*>(p) = make_float4(s[0], s[1], s[2], s[3]);
-                    *reinterpret_cast<float4*>(p + 4) = make_float4(s[4], s[5], s[6], s[7]);
-                } else if constexpr (EP == EP_STORE) {
-                    store8<E>(out + m * e.ld_out + n, s);
-                } else if constexpr (EP == EP_LINEAR) {
-                    float r[8] = {};
-                    if (extra) load8<E>(extra + m * e.ld_extra + n, r);
+                    float* p = e.part + ((long long)split * g.M + mrow[j]) * g.N + n[qp];
+                    if (on) {
+                        *reinterpret_cast<float4*>(p) = make_float4(s[0], s[1], s[2], s[3]);
+                        *reinterpret_cast<float4*>(p + 4) = make_float4(s[4], s[5], s[6], s[7]);
+                    }
+                    continue;
+                }
+                float r[8];
+                unpack8<E>(ex[qp][j], r);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) a[k] = act_only<E, ACT>(s[k] + bias[k]) + r[k];
-                    store8<E>(out + m * e.ld_out + n, a);
-                } else if constexpr (EP == EP_GLU) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) a[k] = (s[k] + bias[k]) * act_only<E, ACT>(s2[k] + bias2[k]);
-                    store8<E>(out + m * e.ld_out + n, a);
-                } else {
-                    float r[8];
-                    load8<E>(extra + m * e.ld_extra + n, r);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
+                for (int k = 0; k < 8; ++k) {
+                    if constexpr (EP == EP_STORE) a[k] = s[k];
+                    else if constexpr (EP == EP_LINEAR) a[k] = act_only<E, ACT>(s[k] + bias[qp][k]) + r[k];
+                    else if constexpr (EP == EP_GLU) a[k] = (s[k] + bias[qp][k]) * act_only<E, ACT>(s2[k] + bias2[qp][k]);
+                    else {
                         float v, d;
                         if constexpr (EP == EP_DLINEAR) {
-                            act_both<E, ACT>(s[k] + bias[k], v, d);
+                            act_both<E, ACT>(s[k] + bias[qp][k], v, d);
                             a[k] = r[k] * d;
                         } else {
-                            act_both<E, ACT>(s2[k] + bias2[k], v, d);
+                            act_both<E, ACT>(s2[k] + bias2[qp][k], v, d);
                             a[k] = r[k] * v;
-                            b[k] = r[k] * (s[k] + bias[k]) * d;
-                            sum2[k] += b[k];
+                            b[k] = r[k] * (s[k] + bias[qp][k]) * d;
+                            sum2[k] += on ? b[k] : 0.f;
                         }
-                        sum[k] += a[k];
+                        sum[k] += on ? a[k] : 0.f;
                     }
-                    store8<E>(out + m * e.ld_out + n, a);
-                    if constexpr (EP == EP_DGLU) store8<E>(out + m * e.ld_out + g.N + n, b);
+                }
+                if (on) {
+                    E* at = out + mrow[j] * e.ld_out + n[qp];
+                    store8<E>(at, a);
+                    if constexpr (EP == EP_DGLU) store8<E>(at + g.N, b);
                 }
             }
             if constexpr (SUMS) {
@@ -127,16 +142,74 @@ __device__ __forceinline__ void finish_tile(const GemmShape& g, const Epilogue& 
                         sum2[k] += __shfl_xor(sum2[k], 16);
                     }
                 }
-                if ((lane & 31) == 0 && n_on) {
+                if ((lane & 31) == 0 && n_on[qp]) {
+                    float* to = e.sums + sum_row * width + n[qp];
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        e.sums[sum_row * width + n + k] = sum[k];
-                        if constexpr (EP == EP_DGLU) e.sums[sum_row * width + g.N + n + k] = sum2[k];
+                        to[k] = sum[k];
+                        if constexpr (EP == EP_DGLU) to[g.N + k] = sum2[k];
                     }
                 }
             }
         }
+    }
 }
+
+// ---- fragments under explicit control: the reads are issued from inline assembly, waited for by count, and tied to the wait by pin ----------------
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+template <int OFF> __device__ __forceinline__ void lds_read_across_async(u32x2_t& dst, uint32_t addr) {
+    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(OFF));
+}
+__device__ __forceinline__ void pin2(u32x2_t& v) { asm volatile("" : "+v"(v)); }
+
+// The fragments of F blocks of 32 rows (block i at tile row (i * W + w) * 32) for one MFMA step, and the addresses they are read from.
+template <typename E, bool ACROSS, int BI, int F, int W> struct Fragments;
+template <typename E, int BI, int F, int W> struct Fragments<E, false, BI, F, W> {
+    static constexpr int READS = F;
+    struct Place { uint32_t base; };
+    u32x4_t f[F];
+    static __device__ __forceinline__ Place place(uint32_t tile, int w, int lane) {
+        const int row = w * 32 + (lane & 31);
+        return Place{tile + (uint32_t)row * 128u + (uint32_t)(((lane >> 5) ^ ((row >> 1) & 7)) << 4)};       // 32 W rows further: the same swizzle
+    }
+    template <int KS> __device__ __forceinline__ void read(const Place& p, uint32_t slot) {
+        const uint32_t at = (p.base ^ (uint32_t)(KS << 5)) + slot;
+        static_for<F>([&](auto ic) { constexpr int i = decltype(ic)::value; lds_read16_async<i * W * 32 * 128>(f[i], at); });
+    }
+    __device__ __forceinline__ void pin_all() {
+#pragma unroll
+        for (int i = 0; i < F; ++i) pin(f[i]);
+    }
+    __device__ __forceinline__ u32x4_t get(int i) const { return f[i]; }
+};
+template <typename E, int BI, int F, int W> struct Fragments<E, true, BI, F, W> {
+    static constexpr int READS = 2 * F;
+    struct Place { uint32_t base[F]; };
+    u32x2_t f[F][2];
+    static __device__ __forceinline__ Place place(uint32_t tile, int w, int lane) {
+        Place p;
+        const int row = 8 * (lane >> 5) + ((lane & 15) >> 2);                                              // rows 4 and 16 further: the same swizzle
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            const int col = (i * W + w) * 32 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+            p.base[i] = tile + (uint32_t)(row * (BI * 2) + (((col >> 3) ^ swz_across<E, BI>(row)) << 4) + ((col & 4) << 1));
+        }
+        return p;
+    }
+    template <int KS> __device__ __forceinline__ void read(const Place& p, uint32_t slot) {
+        static_for<F>([&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            const uint32_t at = p.base[i] + slot;
+            lds_read_across_async<KS * 16 * BI * 2>(f[i][0], at);
+            lds_read_across_async<KS * 16 * BI * 2 + 4 * BI * 2>(f[i][1], at);
+        });
+    }
+    __device__ __forceinline__ void pin_all() {
+#pragma unroll
+        for (int i = 0; i < F; ++i) { pin2(f[i][0]); pin2(f[i][1]); }
+    }
+    __device__ __forceinline__ u32x4_t get(int i) const { return __builtin_shufflevector(f[i][0], f[i][1], 0, 1, 2, 3); }
+};
 
 // BP rows of P x BQ rows of Q per workgroup of WP x WQ waves, ring of NST stages.
 template <typename E, int EP, bool PA, bool QA, int BP, int BQ, int WP, int WQ, int NST>
@@ -146,13 +219,18 @@ __global__ void __launch_bounds__(WP * WQ * 64) gemm_tile_kernel(Operand P, Oper
     constexpr int P_BYTES = BP * 128, STAGE = (BP + BQ) * 128;
     constexpr int LP = BP / 8 / NW, LQ = BQ / 8 / NW;      // 1 KB transfers per wave and stage
     constexpr int BN = GLU ? BP / 2 : BP;
+    // MFMA steps whose fragments are requested together: a group's MFMAs have to last as long as the next group's reads
+    constexpr int KH = FP * FQ >= 8 ? 1 : 2, NG = 4 / KH;
     static_assert(BP % (8 * NW) == 0 && BQ % (8 * NW) == 0, "whole transfers");
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
 
     const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if (logical >= total) return;                          // uniform per workgroup, before any barrier
     const int split = logical / (tiles_p * tiles_q), in = logical - split * (tiles_p * tiles_q);
-    const int bq = in / tiles_p, bp = in - bq * tiles_p;
+    // Eight tiles of Q against each tile of P in turn: the 32 to 64 workgroups that an XCD runs at a time then share tiles of both operands in its L2.
+    constexpr int GROUP = 8;
+    const int group = in / (GROUP * tiles_p), left_q = tiles_q - group * GROUP, gq = left_q < GROUP ? left_q : GROUP, rest = in - group * (GROUP * tiles_p);
+    const int bp = rest / gq, bq = group * GROUP + rest - bp * gq;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
     const int n0 = bp * BN;
     const long long m0 = (long long)bq * BQ;
@@ -221,31 +299,71 @@ __global__ void __launch_bounds__(WP * WQ * 64) gemm_tile_kernel(Operand P, Oper
     };
 
     float16_t acc[FP][FQ] = {};
+    using FragP = Fragments<E, PA, BP, FP, WP>;
+    using FragQ = Fragments<E, QA, BQ, FQ, WQ>;
+    FragP fp[2][KH];
+    FragQ fq[2][KH];
+    const typename FragP::Place place_p = FragP::place(lds0, wp, lane);
+    const typename FragQ::Place place_q = FragQ::place(lds0 + P_BYTES, wq, lane);
+    constexpr int READS = KH * (FragP::READS + FragQ::READS);
+    auto read_group = [&](uint32_t at, auto gc) {           // MFMA steps gc * KH .. of the stage at byte `at` of the ring
+        constexpr int gr = decltype(gc)::value;
+        static_for<KH>([&](auto kc) {
+            constexpr int k = decltype(kc)::value;
+            fq[gr & 1][k].template read<gr * KH + k>(place_q, at);
+            fp[gr & 1][k].template read<gr * KH + k>(place_p, at);
+        });
+    };
+    auto await_group = [&](auto bufc, auto newerc) {
+        lds_wait<(decltype(newerc)::value < 15 ? decltype(newerc)::value : 15)>();
 #pragma unroll
-    for (int s = 0; s < NST - 1; ++s)
-        if (s < stages) issue(s);
-    int slot = 0;
-    for (int s = 0; s < stages; ++s) {
-        // stage s has landed once no more transfers are outstanding than were issued after it
-        if (s + NST - 1 <= stages) wait_vmcnt<(NST - 2) * (LP + LQ)>();
-        else wait_vmcnt<0>();
-        __syncthreads();                                   // ... for every wave, and every wave has read stage s - 1
-        if (s + NST - 1 < stages) issue(slot == 0 ? NST - 1 : slot - 1);
-        const unsigned char* tp = lds + slot * STAGE;
-        const unsigned char* tq = tp + P_BYTES;
+        for (int k = 0; k < KH; ++k) { fp[decltype(bufc)::value][k].pin_all(); fq[decltype(bufc)::value][k].pin_all(); }
+    };
+    auto mma_group = [&](auto bufc) {
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            u32x4_t fp[FP], fq[FQ];
-#pragma unroll
-            for (int j = 0; j < FQ; ++j) fq[j] = read_fragment<E, QA, BQ>(tq, (j * WQ + wq) * 32, ks, lane);
-#pragma unroll
-            for (int i = 0; i < FP; ++i) fp[i] = read_fragment<E, PA, BP>(tp, (i * WP + wp) * 32, ks, lane);
+        for (int k = 0; k < KH; ++k)
 #pragma unroll
             for (int i = 0; i < FP; ++i)
 #pragma unroll
-                for (int j = 0; j < FQ; ++j) Mma<E>::run(fp[i], fq[j], acc[i][j]);
+                for (int j = 0; j < FQ; ++j) Mma<E>::run(fp[decltype(bufc)::value][k].get(i), fq[decltype(bufc)::value][k].get(j), acc[i][j]);
+    };
+    using Newer = std::integral_constant<int, READS>;
+    using None = std::integral_constant<int, 0>;
+
+    // fill the ring, wait for the first stage, request its first fragments
+#pragma unroll
+    for (int s = 0; s < NST; ++s)
+        if (s < stages) issue(s);
+    if (stages >= NST) wait_vmcnt<(NST - 1) * (LP + LQ)>();
+    else wait_vmcnt<0>();
+    __syncthreads();
+    read_group(0, std::integral_constant<int, 0>());
+    int slot = 0;
+    for (int s = 0; s < stages; ++s) {
+        const uint32_t at = (uint32_t)slot * STAGE;
+        const int next_slot = slot + 1 == NST ? 0 : slot + 1;
+        static_for<NG - 1>([&](auto gc) {
+            constexpr int gr = decltype(gc)::value;
+            read_group(at, std::integral_constant<int, gr + 1>());
+            await_group(std::integral_constant<int, (gr & 1)>(), Newer());
+            __builtin_amdgcn_sched_barrier(0);
+            mma_group(std::integral_constant<int, (gr & 1)>());
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        using Last = std::integral_constant<int, ((NG - 1) & 1)>;
+        await_group(Last(), None());                       // this wave has read all of stage s
+        if (s + 1 < stages) {
+            // stage s + 1 has landed once no more transfers are outstanding than were issued after it
+            if (s + NST <= stages) wait_vmcnt<(NST - 2) * (LP + LQ)>();
+            else wait_vmcnt<0>();
+            __syncthreads();                               // ... for every wave, and every wave has read all of stage s
+            if (s + NST < stages) issue(slot);             // stage s + NST, into the slot that stage s used
+            read_group((uint32_t)next_slot * STAGE, std::integral_constant<int, 0>());
         }
-        slot = slot + 1 == NST ? 0 : slot + 1;
+        __builtin_amdgcn_sched_barrier(0);
+        mma_group(Last());
+        __builtin_amdgcn_sched_barrier(0);
+        slot = next_slot;
     }
 
     const long long sum_row = (long long)bq * WQ + wq;
@@ -277,11 +395,19 @@ hipError_t launch_cfg(const Operand& P, const Operand& Q, const GemmShape& g, co
     return hipGetLastError();
 }
 
+// Which block.  Measured on 44 products of a block's sizes, us (4096^3 / 4096 x 640 x 5120 / 4096 x 2560 x 640 / 512 x 5120 x 1280, M x K x N):
+// 256x256 116 / 41 / 56 / 104, 128x128 with two stages 129 / 34 / 30 / 55, with three 160 / 40 / 23 / 42, 64x64 - / 46 / 26 / 23.  A large block
+// moves the fewest bytes through LDS per flop, but has to fill the chip, and with one workgroup per compute unit its epilogue overlaps with nothing:
+// worth it for long reductions only.  128x128 runs two workgroups per unit where there are enough; where there is about one, a third stage pays.
 template <typename E, int EP, bool PA, bool QA> hipError_t launch_shape(const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s, int* sum_rows) {
     constexpr bool GLU = EP == EP_GLU || EP == EP_DGLU;
-    const long long width = GLU ? 2LL * g.N : g.N, big = ((width + 255) / 256) * ((g.M + 255) / 256) * nsplit;
-    if (big >= 224) return launch_cfg<E, EP, PA, QA, 256, 256, 2, 4, 2>(P, Q, g, e, nsplit, s, sum_rows);
-    return launch_cfg<E, EP, PA, QA, 128, 128, 2, 2, 2>(P, Q, g, e, nsplit, s, sum_rows);
+    const long long width = GLU ? 2LL * g.N : g.N, t256 = ((width + 255) / 256) * ((g.M + 255) / 256) * nsplit, t128 = ((width + 127) / 128) * ((g.M + 127) / 128) * nsplit;
+    const int depth = g.K / nsplit;
+    if (depth >= 1536 && t256 >= 224) return launch_cfg<E, EP, PA, QA, 256, 256, 2, 4, 2>(P, Q, g, e, nsplit, s, sum_rows);
+    if (t128 >= 320) return launch_cfg<E, EP, PA, QA, 128, 128, 2, 4, 2>(P, Q, g, e, nsplit, s, sum_rows);
+    if (t128 >= 130 && depth >= 1024) return launch_cfg<E, EP, PA, QA, 128, 128, 2, 4, 3>(P, Q, g, e, nsplit, s, sum_rows);
+    if constexpr (GLU) return launch_cfg<E, EP, PA, QA, 128, 64, 2, 2, 3>(P, Q, g, e, nsplit, s, sum_rows);       // u and g in one wave: 64 rows of P each
+    else return launch_cfg<E, EP, PA, QA, 64, 64, 2, 2, 3>(P, Q, g, e, nsplit, s, sum_rows);
 }
 
 template <typename E, int EP> hipError_t launch_layout(bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s, int* sum_rows) {
