@@ -9,7 +9,92 @@ namespace {
 // Part of a row's result over one range of the keys: o normalised, and the base-2 logarithm of its sum.
 struct AttnParts { float* o; float* lse2; };
 
-template <typename E, int DP> __global__ void __launch_bounds__(256) attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int total, int per_xcd) {
+// Running state of a wave's 32 rows, one per lane and half: the maximum is not followed exactly.  Weights are taken relative to `base`, a multiple of the
+// scores in base 2 that lags behind the true maximum by up to 8: weights stay below 256, far from every type's end, and the sums are rescaled once
+// in many tiles instead of in each.  The result does not depend on base but for rounding.
+template <typename E, int DP> struct AttnState {
+    using T = AttnTile<E, DP>;
+    float16_t acc[T::NV] = {};
+    float base = -INFINITY, l = 0.f;
+
+    // one step over 32 * SUBS streamed keys: scores s (raw), valid keys in the bits of `on` (uniform over the wave)
+    template <int SUBS> __device__ __forceinline__ void weigh(float16_t (&s)[SUBS], unsigned long long on, int half, float c2) {
+        if (on != (SUBS == 2 ? ~0ull : 0xffffffffull)) {
+            asm volatile("" ::: "memory");                 // keeps this a branch: as selects it costs every tile as much as the exponentials
+            const unsigned long long mine = on >> (4 * half);
+#pragma unroll
+            for (int q = 0; q < 16 * SUBS; ++q)
+                if (!((mine >> (32 * (q / 16) + 8 * ((q % 16) / 4) + q % 4)) & 1)) s[q / 16][q % 16] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int q = 1; q < 16 * SUBS; ++q) top = fmaxf(top, s[q / 16][q % 16]);
+        top *= c2;
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__any(top > base + 8.f)) {                     // rows without a key so far: base is -infinity
+            const float next = fmaxf(top, base), f = base == next ? 1.f : __builtin_amdgcn_exp2f(base - next);
+            base = next;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < T::NV; ++d)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) acc[d][q] *= f;
+        }
+        const float shift = base == -INFINITY ? 0.f : base;
+        float sum = 0.f;
+#pragma unroll
+        for (int q = 0; q < 16 * SUBS; ++q) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[q / 16][q % 16], c2, -shift));
+            s[q / 16][q % 16] = p;
+            sum += p;
+        }
+        l += sum;
+    }
+    // base-2 logarithm of the row's sum and the factor that its channels take
+    __device__ __forceinline__ void finish(float& lse2, float& inv) {
+        l += __shfl_xor(l, 32);
+        inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;      // a NaN stays one
+        lse2 = l == 0.f ? -INFINITY : base + log2f(l);
+    }
+};
+
+// One row's channels: to the output, or with several ranges to the parts.
+template <typename E, int DP>
+__device__ __forceinline__ void store_row(const AttnArgs& a, const AttnParts& parts, const AttnRows& rows, int G, int b, int hk, int r, int split, int nsplit, int half,
+                                          const AttnState<E, DP>& st, float inv, float lse2) {
+    using T = AttnTile<E, DP>;
+    const long long row = ((long long)b * a.Hkv + hk) * rows.R + r;
+    if (nsplit > 1) {
+        const long long at = (long long)split * a.B * a.Hkv * rows.R + row;
+        if (half == 0) parts.lse2[at] = lse2;
+        float* o = parts.o + at * a.D;
+#pragma unroll
+        for (int d = 0; d < T::NV; ++d)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = d * 32 + 8 * q + 4 * half;
+                if (c < a.D) *reinterpret_cast<float4*>(o + c) = make_float4(st.acc[d][4 * q] * inv, st.acc[d][4 * q + 1] * inv, st.acc[d][4 * q + 2] * inv, st.acc[d][4 * q + 3] * inv);
+            }
+        return;
+    }
+    if (a.lse && half == 0) a.lse[row] = lse2 * kLn2;
+    unsigned char* orow = const_cast<unsigned char*>(rows.at(a.o, G, b, hk, r, T::ES));
+#pragma unroll
+    for (int d = 0; d < T::NV; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float v[4] = {st.acc[d][4 * q] * inv, st.acc[d][4 * q + 1] * inv, st.acc[d][4 * q + 2] * inv, st.acc[d][4 * q + 3] * inv};
+            store_channels<E>(orow, d * 32 + 8 * q + 4 * half, a.D, v);
+        }
+}
+
+// 128 query rows per workgroup, 32 per wave; keys and values pass through LDS in tiles of 64 while the next tile is on its way in registers.
+// Two waves a SIMD as long as their registers suffice; wide heads give up the tile on its way for that.
+template <typename E, int DP> constexpr int attention_waves() { return DP <= (sizeof(E) == 2 ? 10 : 5) ? 2 : 1; }
+template <typename E, int DP> constexpr int attention_few_waves() { return DP <= (sizeof(E) == 2 ? 6 : 4) ? 2 : 1; }
+template <typename E, int DP> constexpr bool attention_ahead() { return DP <= (sizeof(E) == 2 ? 6 : 4); }
+template <typename E, int DP> __global__ void __launch_bounds__(256, (attention_waves<E, DP>()))
+attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int total, int per_xcd) {
     using T = AttnTile<E, DP>;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     unsigned char* tk = lds;
@@ -23,17 +108,10 @@ template <typename E, int DP> __global__ void __launch_bounds__(256) attention_k
     const int r = tile * 128 + wave * 32 + (lane & 31);
     const bool row_on = r < rows.R;
 
-    u32x4_t fq[T::KS];
-    {
-        const unsigned char* qrow = row_on ? rows.at(a.q, G, b, hk, r, T::ES) : nullptr;
-#pragma unroll
-        for (int ks = 0; ks < T::KS; ++ks) fq[ks] = load_channels<E>(qrow, (2 * ks + half) * T::V, row_on ? a.D : 0);
-    }
     const unsigned char* kbase = static_cast<const unsigned char*>(a.k.p) + ((long long)b * a.k.b + (long long)hk * a.k.h) * T::ES;
     const unsigned char* vbase = static_cast<const unsigned char*>(a.v.p) + ((long long)b * a.v.b + (long long)hk * a.v.h) * T::ES;
     const int len = key_count(a, b), tiles = (len + T::ROWS - 1) / T::ROWS;
     const int t0 = (int)((long long)split * tiles / nsplit), t1 = (int)((long long)(split + 1) * tiles / nsplit);
-
     u32x4_t lk[T::LOADS], lv[T::LOADS];
     auto fetch = [&](int t, unsigned long long on) {
 #pragma unroll
@@ -45,13 +123,20 @@ template <typename E, int DP> __global__ void __launch_bounds__(256) attention_k
             lv[i] = load_channels<E>(vbase + key * a.v.s * T::ES, c, ok ? a.D : 0);
         }
     };
-    float16_t acc[T::NV] = {};
-    float m = -INFINITY, l = 0.f;
-    const float c2 = a.scale * kLog2e;
     unsigned long long next_on = t0 < t1 ? valid_keys(a, b, t0 * T::ROWS, len) : 0;
     if (t0 < t1) fetch(t0, next_on);
+    u32x4_t fq[T::KS];
+    {
+        const unsigned char* qrow = row_on ? rows.at(a.q, G, b, hk, r, T::ES) : nullptr;
+#pragma unroll
+        for (int ks = 0; ks < T::KS; ++ks) fq[ks] = load_channels<E>(qrow, (2 * ks + half) * T::V, row_on ? a.D : 0);
+    }
+    AttnState<E, DP> st;
+    const float c2 = a.scale * kLog2e;
+    constexpr bool AHEAD = attention_ahead<E, DP>();
     for (int t = t0; t < t1; ++t) {
         const unsigned long long on = next_on;
+        if (!AHEAD && t > t0) fetch(t, on);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < T::LOADS; ++i) {
@@ -65,7 +150,7 @@ template <typename E, int DP> __global__ void __launch_bounds__(256) attention_k
         __syncthreads();
         if (t + 1 < t1) {
             next_on = valid_keys(a, b, (t + 1) * T::ROWS, len);
-            fetch(t + 1, next_on);
+            if (AHEAD) fetch(t + 1, next_on);
         }
         if (on == 0) continue;                             // uniform: every wave has the same keys
         float16_t s[2] = {};
@@ -73,68 +158,132 @@ template <typename E, int DP> __global__ void __launch_bounds__(256) attention_k
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int ks = 0; ks < T::KS; ++ks) Mma<E>::run(T::along(tk, 32 * i, ks, lane), fq[ks], s[i]);
-        if (on != ~0ull) {
-            const unsigned long long mine = on >> (4 * half);
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int q = 0; q < 16; ++q)
-                    if (!((mine >> (32 * i + 8 * (q / 4) + q % 4)) & 1)) s[i][q] = -INFINITY;
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int q = 1; q < 32; ++q) top = fmaxf(top, s[q / 16][q % 16]);
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float m_new = fmaxf(m, top * c2), base = m_new == -INFINITY ? 0.f : m_new, alpha = __builtin_amdgcn_exp2f(m - base);
-        m = m_new;
-        float sum = 0.f;
-#pragma unroll
-        for (int q = 0; q < 32; ++q) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[q / 16][q % 16], c2, -base));
-            s[q / 16][q % 16] = p;
-            sum += p;
-        }
-        l = fmaf(l, alpha, sum);
-#pragma unroll
-        for (int d = 0; d < T::NV; ++d)
-#pragma unroll
-            for (int q = 0; q < 16; ++q) acc[d][q] *= alpha;
+        st.template weigh<2>(s, on, half, c2);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int st = 0; st < T::ST; ++st) {
-                const u32x4_t w = T::weights(s[i], st);
+            for (int k = 0; k < T::ST; ++k) {
+                const u32x4_t w = T::weights(s[i], k);
 #pragma unroll
-                for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(tv, 32 * i, st, d, lane), w, acc[d]);
+                for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(tv, 32 * i, k, d, lane), w, st.acc[d]);
             }
     }
-    l += __shfl_xor(l, 32);
-    if (!row_on) return;
-    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;           // a NaN stays one
-    const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
-    const long long row = (long long)bh * rows.R + r;
-    if (nsplit > 1) {
-        const long long all = (long long)a.B * a.Hkv * rows.R, at = (long long)split * all + row;
-        if (half == 0) parts.lse2[at] = lse2;
-        float* o = parts.o + at * a.D;
+    float lse2, inv;
+    st.finish(lse2, inv);
+    if (row_on) store_row<E, DP>(a, parts, rows, G, b, hk, r, split, nsplit, half, st, inv, lse2);
+}
+
+// At most 32 query rows a key head (one token of each query head that shares it, say): the four waves of a workgroup take different keys for the same
+// rows and are joined in LDS.  Bound by reading the keys: a wave's scores take them straight from memory, only the values, which the second
+// product needs across, pass through LDS of the wave's own; no barrier in the loop.
+template <typename E, int DP> __global__ void __launch_bounds__(256, (attention_few_waves<E, DP>()))
+attention_few_kernel(AttnArgs a, AttnParts parts, int nsplit, int total, int per_xcd) {
+    using T = AttnTile<E, DP>;
+    constexpr int KEYS = 32, WAVE_BYTES = KEYS * T::STRIDE, LOADS = (KEYS * T::CPR + 63) / 64;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+    if (logical >= total) return;
+    const int bh = logical / nsplit, split = logical - bh * nsplit;
+    const int b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
+    const AttnRows rows{a.Sq, G * a.Sq};
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int r = lane & 31;
+    const bool row_on = r < rows.R;
+    unsigned char* tv = lds + wave * WAVE_BYTES;
+
+    const unsigned char* kbase = static_cast<const unsigned char*>(a.k.p) + ((long long)b * a.k.b + (long long)hk * a.k.h) * T::ES;
+    const unsigned char* vbase = static_cast<const unsigned char*>(a.v.p) + ((long long)b * a.v.b + (long long)hk * a.v.h) * T::ES;
+    const int len = key_count(a, b), tiles = (len + KEYS - 1) / KEYS, part = split * 4 + wave;
+    const int t0 = (int)((long long)part * tiles / (nsplit * 4)), t1 = (int)((long long)(part + 1) * tiles / (nsplit * 4));
+    u32x4_t fq[T::KS], fk[T::KS], lv[LOADS];
+    {
+        const unsigned char* qrow = row_on ? rows.at(a.q, G, b, hk, r, T::ES) : nullptr;
+#pragma unroll
+        for (int ks = 0; ks < T::KS; ++ks) fq[ks] = load_channels<E>(qrow, (2 * ks + half) * T::V, row_on ? a.D : 0);
+    }
+    auto mask = [&](int t) { return valid_keys(a, b, t * KEYS, len) & 0xffffffffull; };
+    auto fetch_keys = [&](int t, unsigned long long on) {
+        const bool ok = (on >> r) & 1;
+        const unsigned char* row = kbase + ((long long)t * KEYS + r) * a.k.s * T::ES;
+#pragma unroll
+        for (int ks = 0; ks < T::KS; ++ks) fk[ks] = load_channels<E>(row, (2 * ks + half) * T::V, ok ? a.D : 0);
+    };
+    auto fetch_values = [&](int t, unsigned long long on) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int id = lane + 64 * i, row = id / T::CPR, c = (id - row * T::CPR) * T::V;
+            const bool ok = row < KEYS && ((on >> (row & 31)) & 1);
+            lv[i] = load_channels<E>(vbase + ((long long)t * KEYS + row) * a.v.s * T::ES, c, ok ? a.D : 0);
+        }
+    };
+    AttnState<E, DP> st;
+    const float c2 = a.scale * kLog2e;
+    unsigned long long on = t0 < t1 ? mask(t0) : 0;
+    if (t0 < t1) { fetch_keys(t0, on); fetch_values(t0, on); }
+    for (int t = t0; t < t1; ++t) {
+        const unsigned long long cur = on;
+        float16_t s[1] = {};
+#pragma unroll
+        for (int ks = 0; ks < T::KS; ++ks) Mma<E>::run(fk[ks], fq[ks], s[0]);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int id = lane + 64 * i, row = id / T::CPR;
+            if (row < KEYS) *reinterpret_cast<u32x4_t*>(tv + T::at(row, id - row * T::CPR)) = lv[i];
+        }
+        if (t + 1 < t1) {
+            on = mask(t + 1);
+            fetch_keys(t + 1, on);
+            fetch_values(t + 1, on);
+        }
+        if (cur == 0) continue;                            // uniform over the wave
+        st.template weigh<1>(s, cur, half, c2);
+        __builtin_amdgcn_wave_barrier();                   // the values of this tile are in LDS: written and read by this wave, in order
+#pragma unroll
+        for (int k = 0; k < T::ST; ++k) {
+            const u32x4_t w = T::weights(s[0], k);
+#pragma unroll
+            for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(tv, 0, k, d, lane), w, st.acc[d]);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    // join the four waves: each leaves base, sum and channels; wave 0 adds them up in order
+    st.l += __shfl_xor(st.l, 32);
+    __syncthreads();
+    constexpr int ROW = T::NV * 32 + 2;                    // floats per row and wave: channels, base, sum
+    float* mine = reinterpret_cast<float*>(lds) + (wave * 32 + r) * (ROW + 1);
+    if (row_on) {
 #pragma unroll
         for (int d = 0; d < T::NV; ++d)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int c = d * 32 + 8 * q + 4 * half;
-                if (c < a.D) *reinterpret_cast<float4*>(o + c) = make_float4(acc[d][4 * q] * inv, acc[d][4 * q + 1] * inv, acc[d][4 * q + 2] * inv, acc[d][4 * q + 3] * inv);
-            }
-        return;
+            for (int q = 0; q < 16; ++q) mine[d * 32 + 8 * (q / 4) + 4 * half + q % 4] = st.acc[d][q];
+        if (half == 0) { mine[T::NV * 32] = st.base; mine[T::NV * 32 + 1] = st.l; }
     }
-    if (a.lse && half == 0) a.lse[row] = lse2 * kLn2;
-    unsigned char* orow = const_cast<unsigned char*>(rows.at(a.o, G, b, hk, r, T::ES));
+    __syncthreads();
+    if (wave != 0 || !row_on) return;
+    const float* all = reinterpret_cast<const float*>(lds) + r * (ROW + 1);
+    constexpr int STEP = 32 * (ROW + 1);
+    float base = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) base = fmaxf(base, all[w * STEP + T::NV * 32]);
+    const float shift = base == -INFINITY ? 0.f : base;
+    float l = 0.f, f[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        f[w] = __builtin_amdgcn_exp2f(all[w * STEP + T::NV * 32] - shift);
+        l = fmaf(all[w * STEP + T::NV * 32 + 1], f[w], l);
+    }
 #pragma unroll
     for (int d = 0; d < T::NV; ++d)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float v[4] = {acc[d][4 * q] * inv, acc[d][4 * q + 1] * inv, acc[d][4 * q + 2] * inv, acc[d][4 * q + 3] * inv};
-            store_channels<E>(orow, d * 32 + 8 * q + 4 * half, a.D, v);
+        for (int q = 0; q < 16; ++q) {
+            const int c = d * 32 + 8 * (q / 4) + 4 * half + q % 4;
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) v = fmaf(all[w * STEP + c], f[w], v);
+            st.acc[d][q] = v;
         }
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l, lse2 = l == 0.f ? -INFINITY : base + log2f(l);
+    store_row<E, DP>(a, parts, rows, G, b, hk, r, split, nsplit, half, st, inv, lse2);
 }
 
 // one wave per row: the ranges' results, weighted by their sums
@@ -159,12 +308,17 @@ template <typename E> __global__ void __launch_bounds__(256) attention_join_kern
     if (a.lse && lane == 0) a.lse[row] = total == 0.f ? -INFINITY : (m + log2f(total)) * kLn2;
 }
 
-// Ranges of the keys, where the rows alone leave compute units idle: up to two workgroups a unit, at least four tiles a range.
+// Whether the rows of a key head fit one wave's tile.
+bool few_rows(int Sq, int H, int Hkv) { return (long long)(H / Hkv) * Sq <= 32; }
+
+// Ranges of the keys, where the rows alone leave compute units idle: about two workgroups a unit (few rows: four, because lengths that differ leave
+// some of them short), at least 256 keys a range (few rows: 128 a wave).
 int attention_ranges(int B, int Sq, int Skv, int H, int Hkv) {
-    const long long blocks = (long long)B * Hkv * (((long long)(H / Hkv) * Sq + 127) / 128);
-    const int tiles = (Skv + 63) / 64;
-    long long n = 512 / blocks;
-    if (n > tiles / 4) n = tiles / 4;
+    const bool few = few_rows(Sq, H, Hkv);
+    const long long blocks = few ? (long long)B * Hkv : (long long)B * Hkv * (((long long)(H / Hkv) * Sq + 127) / 128);
+    long long n = (few ? 1024 : 512) / blocks;
+    const int most = Skv / (few ? 512 : 256);
+    if (n > most) n = most;
     if (n > 64) n = 64;
     return n < 2 ? 1 : (int)n;
 }
@@ -190,6 +344,16 @@ hipError_t launch_attention(const AttnArgs& a, int dt, hipStream_t s) {
             if constexpr (sizeof(E) == 4 && DP > 10) return hipErrorInvalidValue;
             else {
                 using T = AttnTile<E, DP>;
+                if (few_rows(a.Sq, a.H, a.Hkv)) {
+                    auto kern = attention_few_kernel<E, DP>;
+                    constexpr int tiles = 4 * 32 * T::STRIDE, joined = 4 * 32 * (T::NV * 32 + 3) * 4, bytes = tiles > joined ? tiles : joined;
+                    static_assert(bytes <= 160 * 1024, "LDS budget");
+                    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+                    if (attr != hipSuccess) return attr;
+                    const int count = a.B * a.Hkv * nsplit, each = (count + 7) / 8;
+                    hipLaunchKernelGGL(kern, dim3((unsigned)(each * 8)), dim3(256), bytes, s, a, parts, nsplit, count, each);
+                    return hipGetLastError();
+                }
                 auto kern = attention_kernel<E, DP>;
                 constexpr int bytes = 2 * T::BYTES;
                 static_assert(bytes <= 160 * 1024, "LDS budget");

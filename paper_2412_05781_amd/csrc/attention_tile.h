@@ -14,6 +14,19 @@ namespace wino {
 typedef short attn_s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) attn_s16x4_t attn_lds_s16x4_t;
 
+// two neighbouring weights or results in one word, rounded to nearest even (one instruction, where two conversions and a merge take four)
+template <typename E> __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    const f32x2 v = {a, b};
+    if constexpr (std::is_same_v<E, bf16_t>) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+    } else {
+        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+    }
+}
+
 // DP: channels / 16, rounded up
 template <typename E, int DP> struct AttnTile {
     static constexpr int ES = (int)sizeof(E);
@@ -62,7 +75,7 @@ template <typename E, int DP> struct AttnTile {
         u32x4_t f;
         if constexpr (ES == 2) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = pack2<E>(p[8 * st + 2 * j], p[8 * st + 2 * j + 1]);
+            for (int j = 0; j < 4; ++j) f[j] = pack_pair<E>(p[8 * st + 2 * j], p[8 * st + 2 * j + 1]);
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) f[j] = __float_as_uint(p[4 * st + j]);
@@ -90,7 +103,7 @@ template <typename E> __device__ __forceinline__ u32x4_t load_channels(const uns
 template <typename E> __device__ __forceinline__ void store_channels(unsigned char* row, int c, int D, const float* v) {
     if (c >= D) return;
     if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(row + c * 4) = make_float4(v[0], v[1], v[2], v[3]);
-    else *reinterpret_cast<uint2*>(row + c * 2) = make_uint2(pack2<E>(v[0], v[1]), pack2<E>(v[2], v[3]));
+    else *reinterpret_cast<uint2*>(row + c * 2) = make_uint2(pack_pair<E>(v[0], v[1]), pack_pair<E>(v[2], v[3]));
 }
 
 // Valid keys among the 64 from key0 on, one bit each: below the row's length and not masked.  Called by whole waves.
