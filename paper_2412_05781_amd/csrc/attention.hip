@@ -17,8 +17,8 @@ template <typename E, int DP> struct AttnState {
     float16_t acc[T::NV] = {};
     float base = -INFINITY, l = 0.f;
 
-    // one step over 32 * SUBS streamed keys: scores s (raw), valid keys in the bits of `on` (uniform over the wave)
-    template <int SUBS> __device__ __forceinline__ void weigh(float16_t (&s)[SUBS], unsigned long long on, int half, float c2) {
+    // takes the scores of 32 * SUBS streamed keys (raw; valid keys in the bits of `on`, uniform over the wave) into account for the base
+    template <int SUBS> __device__ __forceinline__ void settle(float16_t (&s)[SUBS], unsigned long long on, int half, float c2) {
         if (on != (SUBS == 2 ? ~0ull : 0xffffffffull)) {
             asm volatile("" ::: "memory");                 // keeps this a branch: as selects it costs every tile as much as the exponentials
             const unsigned long long mine = on >> (4 * half);
@@ -40,12 +40,15 @@ template <typename E, int DP> struct AttnState {
 #pragma unroll
                 for (int q = 0; q < 16; ++q) acc[d][q] *= f;
         }
-        const float shift = base == -INFINITY ? 0.f : base;
+    }
+    __device__ __forceinline__ float shift() const { return base == -INFINITY ? 0.f : base; }
+    // scores to weights
+    __device__ __forceinline__ void weigh(float16_t& s, float c2, float sh) {
         float sum = 0.f;
 #pragma unroll
-        for (int q = 0; q < 16 * SUBS; ++q) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[q / 16][q % 16], c2, -shift));
-            s[q / 16][q % 16] = p;
+        for (int q = 0; q < 16; ++q) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[q], c2, -sh));
+            s[q] = p;
             sum += p;
         }
         l += sum;
@@ -92,13 +95,11 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, const AttnParts& pa
 // Two waves a SIMD as long as their registers suffice; wide heads give up the tile on its way for that.
 template <typename E, int DP> constexpr int attention_waves() { return DP <= (sizeof(E) == 2 ? 10 : 5) ? 2 : 1; }
 template <typename E, int DP> constexpr int attention_few_waves() { return DP <= (sizeof(E) == 2 ? 6 : 4) ? 2 : 1; }
-template <typename E, int DP> constexpr bool attention_ahead() { return DP <= (sizeof(E) == 2 ? 6 : 4); }
+template <typename E, int DP> constexpr bool attention_ahead() { return sizeof(E) == 2 && DP <= 6; }
 template <typename E, int DP> __global__ void __launch_bounds__(256, (attention_waves<E, DP>()))
 attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int total, int per_xcd) {
     using T = AttnTile<E, DP>;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    unsigned char* tk = lds;
-    unsigned char* tv = lds + T::BYTES;
     const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if (logical >= total) return;
     const int per_head = row_tiles * nsplit, bh = logical / per_head, in = logical - bh * per_head, split = in / row_tiles, tile = in - split * row_tiles;
@@ -112,61 +113,73 @@ attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int tot
     const unsigned char* vbase = static_cast<const unsigned char*>(a.v.p) + ((long long)b * a.v.b + (long long)hk * a.v.h) * T::ES;
     const int len = key_count(a, b), tiles = (len + T::ROWS - 1) / T::ROWS;
     const int t0 = (int)((long long)split * tiles / nsplit), t1 = (int)((long long)(split + 1) * tiles / nsplit);
-    u32x4_t lk[T::LOADS], lv[T::LOADS];
-    auto fetch = [&](int t, unsigned long long on) {
-#pragma unroll
-        for (int i = 0; i < T::LOADS; ++i) {
-            const int id = tid + 256 * i, row = id / T::CPR, c = (id - row * T::CPR) * T::V;
-            const bool ok = row < T::ROWS && ((on >> (row & 63)) & 1);
-            const long long key = (long long)t * T::ROWS + row;
-            lk[i] = load_channels<E>(kbase + key * a.k.s * T::ES, c, ok ? a.D : 0);
-            lv[i] = load_channels<E>(vbase + key * a.v.s * T::ES, c, ok ? a.D : 0);
-        }
-    };
-    unsigned long long next_on = t0 < t1 ? valid_keys(a, b, t0 * T::ROWS, len) : 0;
-    if (t0 < t1) fetch(t0, next_on);
+    using Stream = AttnStream<E, DP>;
+    const typename Stream::Map map(tid, a.D);
+    Stream sk(map, kbase, t0 * T::ROWS, a.k.s), sv(map, vbase, t0 * T::ROWS, a.v.s);
     u32x4_t fq[T::KS];
-    {
+    auto load_rows = [&] {
         const unsigned char* qrow = row_on ? rows.at(a.q, G, b, hk, r, T::ES) : nullptr;
 #pragma unroll
         for (int ks = 0; ks < T::KS; ++ks) fq[ks] = load_channels<E>(qrow, (2 * ks + half) * T::V, row_on ? a.D : 0);
-    }
+    };
     AttnState<E, DP> st;
     const float c2 = a.scale * kLog2e;
-    constexpr bool AHEAD = attention_ahead<E, DP>();
-    for (int t = t0; t < t1; ++t) {
-        const unsigned long long on = next_on;
-        if (!AHEAD && t > t0) fetch(t, on);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < T::LOADS; ++i) {
-            const int id = tid + 256 * i, row = id / T::CPR;
-            if (row < T::ROWS) {
-                const int at = T::at(row, id - row * T::CPR);
-                *reinterpret_cast<u32x4_t*>(tk + at) = lk[i];
-                *reinterpret_cast<u32x4_t*>(tv + at) = lv[i];
-            }
-        }
-        __syncthreads();
-        if (t + 1 < t1) {
-            next_on = valid_keys(a, b, (t + 1) * T::ROWS, len);
-            if (AHEAD) fetch(t + 1, next_on);
-        }
-        if (on == 0) continue;                             // uniform: every wave has the same keys
+    auto valid = [&](int t) { return t < t1 ? valid_keys(a, b, t * T::ROWS, len) : 0ull; };
+    auto step = [&](const unsigned char* tk, const unsigned char* tv, unsigned long long on) {
         float16_t s[2] = {};
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int ks = 0; ks < T::KS; ++ks) Mma<E>::run(T::along(tk, 32 * i, ks, lane), fq[ks], s[i]);
-        st.template weigh<2>(s, on, half, c2);
+        st.template settle<2>(s, on, half, c2);
+        const float sh = st.shift();
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 2; ++i) {
+            st.weigh(s[i], c2, sh);
 #pragma unroll
             for (int k = 0; k < T::ST; ++k) {
                 const u32x4_t w = T::weights(s[i], k);
 #pragma unroll
                 for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(tv, 32 * i, k, d, lane), w, st.acc[d]);
             }
+        }
+    };
+    if constexpr (attention_ahead<E, DP>()) {
+        // two buffers in turn, one barrier a tile
+        unsigned long long on = valid(t0);
+        if (t0 < t1) {
+            sk.fetch(map, on);
+            sv.fetch(map, on);
+        }
+        load_rows();
+        for (int t = t0; t < t1; ++t) {
+            unsigned char* tk = lds + ((t - t0) & 1) * 2 * T::BYTES;
+            unsigned char* tv = tk + T::BYTES;
+            sk.put(map, tk);
+            sv.put(map, tv);
+            __syncthreads();
+            const unsigned long long cur = on;
+            if (t + 1 < t1) {
+                on = valid(t + 1);
+                sk.fetch(map, on);
+                sv.fetch(map, on);
+            }
+            if (cur) step(tk, tv, cur);                    // uniform: every wave has the same keys
+        }
+    } else {
+        unsigned char* tk = lds;
+        unsigned char* tv = lds + T::BYTES;
+        load_rows();
+        for (int t = t0; t < t1; ++t) {
+            const unsigned long long on = valid(t);
+            sk.fetch(map, on);
+            sv.fetch(map, on);
+            __syncthreads();
+            sk.put(map, tk);
+            sv.put(map, tv);
+            __syncthreads();
+            if (on) step(tk, tv, on);
+        }
     }
     float lse2, inv;
     st.finish(lse2, inv);
@@ -236,7 +249,8 @@ attention_few_kernel(AttnArgs a, AttnParts parts, int nsplit, int total, int per
             fetch_values(t + 1, on);
         }
         if (cur == 0) continue;                            // uniform over the wave
-        st.template weigh<1>(s, cur, half, c2);
+        st.template settle<1>(s, cur, half, c2);
+        st.weigh(s[0], c2, st.shift());
         __builtin_amdgcn_wave_barrier();                   // the values of this tile are in LDS: written and read by this wave, in order
 #pragma unroll
         for (int k = 0; k < T::ST; ++k) {
@@ -355,7 +369,7 @@ hipError_t launch_attention(const AttnArgs& a, int dt, hipStream_t s) {
                     return hipGetLastError();
                 }
                 auto kern = attention_kernel<E, DP>;
-                constexpr int bytes = 2 * T::BYTES;
+                constexpr int bytes = (attention_ahead<E, DP>() ? 4 : 2) * T::BYTES;
                 static_assert(bytes <= 160 * 1024, "LDS budget");
                 static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
                 if (attr != hipSuccess) return attr;

@@ -1,8 +1,9 @@
 // Gradients of attention.  With p = exp(s - lse) from the forward pass and D_i = do_i . o_i:
 //   dv = p^T do,  ds = p (do v^T - D),  dq = scale ds k,  dk = scale ds^T q.
 // Scores are made again, never stored.  Two kernels, both without atomics, so that results do not depend on the order of the workgroups: one owns
-// 128 query rows and streams the keys (dq), one owns 128 keys and streams the query rows of their head (dk, dv; over ranges of the rows, joined in
-// order, where there are few keys).
+// 64 query rows and streams the keys (dq, and D for the other), one owns 64 keys and streams the query rows of their head (dk, dv; over ranges of
+// the rows, joined in order, where there are few keys).  In either, two waves own 32 rows or keys each and the other two the same ones against the
+// other half of every streamed tile; the halves are added in LDS at the end.
 #include "attention_tile.h"
 
 namespace wino {
@@ -15,98 +16,123 @@ struct BackwardParts {
     float* dv;
 };
 
-// D_i = do_i . o_i, sixteen lanes a row
-template <typename E> __global__ void __launch_bounds__(256) attention_delta_kernel(AttnArgs a, float* delta, long long all) {
-    const long long row = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
-    const int lane = threadIdx.x & 15, G = a.H / a.Hkv;
-    if (row >= all) return;                                // whole groups of sixteen lanes leave together
-    const AttnRows rows{a.Sq, G * a.Sq};
-    const int bh = (int)(row / rows.R), r = (int)(row - (long long)bh * rows.R), b = bh / a.Hkv, hk = bh - b * a.Hkv;
-    const unsigned char* o = rows.at(a.o, G, b, hk, r, (int)sizeof(E));
-    const unsigned char* d = rows.at(a.dout, G, b, hk, r, (int)sizeof(E));
-    constexpr int V = 16 / (int)sizeof(E);
-    float t = 0.f;
-    for (int c = lane * V; c < a.D; c += 16 * V) {
-        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(o + c * (int)sizeof(E)), y = *reinterpret_cast<const u32x4_t*>(d + c * (int)sizeof(E));
+// Two waves a SIMD as long as their registers suffice.
+template <typename E, int DP> constexpr int backward_waves() { return DP <= (sizeof(E) == 2 ? 6 : 4) ? 2 : 1; }
+// Two-byte types keep two tiles in LDS and one on its way; fp32's tiles are too large for that.
+template <typename E> constexpr bool backward_ahead() { return sizeof(E) == 2; }
+
+// adds the accumulators of waves 2 and 3 to those of waves 0 and 1, through LDS; called by the whole workgroup
+template <int N> __device__ __forceinline__ void add_halves(float16_t (&acc)[N], unsigned char* lds, int wave, int lane) {
+    float* t = reinterpret_cast<float*>(lds) + (wave & 1) * (N * 1024) + lane;
+    __syncthreads();
+    if (wave >= 2) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(E) == 4) t = fmaf(__uint_as_float(x[i]), __uint_as_float(y[i]), t);
-            else { t = fmaf(lo16<E>(x[i]), lo16<E>(y[i]), t); t = fmaf(hi16<E>(x[i]), hi16<E>(y[i]), t); }
-        }
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) t[(d * 16 + q) * 64] = acc[d][q];
     }
+    __syncthreads();
+    if (wave < 2) {
 #pragma unroll
-    for (int k = 8; k; k >>= 1) t += __shfl_xor(t, k, 16);
-    if (lane == 0) delta[row] = t;
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[d][q] += t[(d * 16 + q) * 64];
+    }
 }
 
-template <typename E, int DP> __global__ void __launch_bounds__(256) attention_dq_kernel(AttnArgs a, const float* delta, int row_tiles, int total, int per_xcd) {
+// 64 query rows: dq, and D_i on the way
+template <typename E, int DP> __global__ void __launch_bounds__(256, (backward_waves<E, DP>()))
+attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_xcd) {
     using T = AttnTile<E, DP>;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    unsigned char* tk = lds;
-    unsigned char* tv = lds + T::BYTES;
     const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if (logical >= total) return;
     const int bh = logical / row_tiles, tile = logical - bh * row_tiles, b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
     const AttnRows rows{a.Sq, G * a.Sq};
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-    const int r = tile * 128 + wave * 32 + (lane & 31);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, sub = wave >> 1;
+    const int r = tile * 64 + (wave & 1) * 32 + (lane & 31);
     const bool row_on = r < rows.R;
-    u32x4_t fq[T::KS], fo[T::KS];
-    {
-        const unsigned char* qrow = row_on ? rows.at(a.q, G, b, hk, r, T::ES) : nullptr;
-        const unsigned char* orow = row_on ? rows.at(a.dout, G, b, hk, r, T::ES) : nullptr;
-#pragma unroll
-        for (int ks = 0; ks < T::KS; ++ks) {
-            fq[ks] = load_channels<E>(qrow, (2 * ks + half) * T::V, row_on ? a.D : 0);
-            fo[ks] = load_channels<E>(orow, (2 * ks + half) * T::V, row_on ? a.D : 0);
-        }
-    }
-    const long long row = (long long)bh * rows.R + r;
-    const float lse2 = row_on ? a.lse[row] * kLog2e : 0.f, dlt = row_on ? delta[row] : 0.f;
     const unsigned char* kbase = static_cast<const unsigned char*>(a.k.p) + ((long long)b * a.k.b + (long long)hk * a.k.h) * T::ES;
     const unsigned char* vbase = static_cast<const unsigned char*>(a.v.p) + ((long long)b * a.v.b + (long long)hk * a.v.h) * T::ES;
     const int len = key_count(a, b), tiles = (len + T::ROWS - 1) / T::ROWS;
+    using Stream = AttnStream<E, DP>;
+    const typename Stream::Map map(tid, a.D);
+    Stream sk(map, kbase, 0, a.k.s), sv(map, vbase, 0, a.v.s);
+    constexpr bool AHEAD = backward_ahead<E>();
+    unsigned long long on = tiles ? valid_keys(a, b, 0, len) : 0;
+    if (AHEAD && tiles) {
+        sk.fetch(map, on);
+        sv.fetch(map, on);
+    }
+    u32x4_t fq[T::KS], fo[T::KS];
+    const long long row = (long long)bh * rows.R + r;
+    float dlt = 0.f;
+    {
+        const unsigned char* qrow = row_on ? rows.at(a.q, G, b, hk, r, T::ES) : nullptr;
+        const unsigned char* grow = row_on ? rows.at(a.dout, G, b, hk, r, T::ES) : nullptr;
+        const unsigned char* orow = row_on ? rows.at(a.o, G, b, hk, r, T::ES) : nullptr;
+#pragma unroll
+        for (int ks = 0; ks < T::KS; ++ks) {
+            const int c = (2 * ks + half) * T::V, D = row_on ? a.D : 0;
+            fq[ks] = load_channels<E>(qrow, c, D);
+            fo[ks] = load_channels<E>(grow, c, D);
+            const u32x4_t x = load_channels<E>(orow, c, D);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (T::ES == 4) dlt = fmaf(__uint_as_float(x[i]), __uint_as_float(fo[ks][i]), dlt);
+                else { dlt = fmaf(lo16<E>(x[i]), lo16<E>(fo[ks][i]), dlt); dlt = fmaf(hi16<E>(x[i]), hi16<E>(fo[ks][i]), dlt); }
+            }
+        }
+        dlt += __shfl_xor(dlt, 32);
+        if (row_on && sub == 0 && half == 0) delta[row] = dlt;
+    }
+    const float lse2 = row_on ? a.lse[row] * kLog2e : 0.f;
     float16_t acc[T::NV] = {};
     const float c2 = a.scale * kLog2e;
     for (int t = 0; t < tiles; ++t) {
-        const unsigned long long on = valid_keys(a, b, t * T::ROWS, len);
-        if (on == 0) continue;                             // uniform
+        unsigned char* tk = lds + (AHEAD ? (t & 1) * 2 * T::BYTES : 0);
+        unsigned char* tv = tk + T::BYTES;
+        if (!AHEAD) {
+            sk.fetch(map, on);
+            sv.fetch(map, on);
+            __syncthreads();
+        }
+        sk.put(map, tk);
+        sv.put(map, tv);
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < T::LOADS; ++i) {
-            const int id = tid + 256 * i, kr = id / T::CPR, ch = id - kr * T::CPR;
-            if (kr < T::ROWS) {
-                const bool ok = (on >> kr) & 1;
-                const long long key = (long long)t * T::ROWS + kr;
-                *reinterpret_cast<u32x4_t*>(tk + T::at(kr, ch)) = load_channels<E>(kbase + key * a.k.s * T::ES, ch * T::V, ok ? a.D : 0);
-                *reinterpret_cast<u32x4_t*>(tv + T::at(kr, ch)) = load_channels<E>(vbase + key * a.v.s * T::ES, ch * T::V, ok ? a.D : 0);
+        const uint32_t cur = (uint32_t)(on >> (32 * sub));
+        if (t + 1 < tiles) {
+            on = valid_keys(a, b, (t + 1) * T::ROWS, len);
+            if (AHEAD) {
+                sk.fetch(map, on);
+                sv.fetch(map, on);
             }
         }
-        __syncthreads();
-        const unsigned long long mine = on >> (4 * half);
+        if (cur == 0) continue;                            // uniform over the wave
+        float16_t s = {}, dp = {};
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            float16_t s = {}, dp = {};
+        for (int ks = 0; ks < T::KS; ++ks) {
+            Mma<E>::run(T::along(tk, 32 * sub, ks, lane), fq[ks], s);
+            Mma<E>::run(T::along(tv, 32 * sub, ks, lane), fo[ks], dp);
+        }
 #pragma unroll
-            for (int ks = 0; ks < T::KS; ++ks) {
-                Mma<E>::run(T::along(tk, 32 * i, ks, lane), fq[ks], s);
-                Mma<E>::run(T::along(tv, 32 * i, ks, lane), fo[ks], dp);
-            }
+        for (int q = 0; q < 16; ++q) s[q] = __builtin_amdgcn_exp2f(fmaf(s[q], c2, -lse2)) * (dp[q] - dlt);
+        if (cur != 0xffffffffu) {
+            asm volatile("" ::: "memory");                 // a branch
+            const uint32_t mine = cur >> (4 * half);
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-                const bool ok = (mine >> (32 * i + 8 * (q / 4) + q % 4)) & 1;
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[q], c2, -lse2));
-                s[q] = ok ? p * (dp[q] - dlt) : 0.f;
-            }
+            for (int q = 0; q < 16; ++q)
+                if (!((mine >> (8 * (q / 4) + q % 4)) & 1)) s[q] = 0.f;
+        }
 #pragma unroll
-            for (int st = 0; st < T::ST; ++st) {
-                const u32x4_t w = T::weights(s, st);
+        for (int st = 0; st < T::ST; ++st) {
+            const u32x4_t w = T::weights(s, st);
 #pragma unroll
-                for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(tk, 32 * i, st, d, lane), w, acc[d]);
-            }
+            for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(tk, 32 * sub, st, d, lane), w, acc[d]);
         }
     }
-    if (!row_on) return;
+    add_halves<T::NV>(acc, lds, wave, lane);
+    if (sub || !row_on) return;
     unsigned char* out = const_cast<unsigned char*>(rows.at(a.dq, G, b, hk, r, T::ES));
 #pragma unroll
     for (int d = 0; d < T::NV; ++d)
@@ -117,24 +143,51 @@ template <typename E, int DP> __global__ void __launch_bounds__(256) attention_d
         }
 }
 
-template <typename E, int DP> __global__ void __launch_bounds__(256) attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit, int total, int per_xcd) {
+// 64 keys: dk and dv over one range of the query rows.  Tiles hold rows of one query head each.
+template <typename E, int DP> __global__ void __launch_bounds__(256, (backward_waves<E, DP>()))
+attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit, int total, int per_xcd) {
     using T = AttnTile<E, DP>;
+    constexpr bool AHEAD = backward_ahead<E>();
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    unsigned char* tq = lds;
-    unsigned char* to = lds + T::BYTES;
-    float* tl = reinterpret_cast<float*>(lds + 2 * T::BYTES);          // lse and delta of the tile's rows
-    float* td = tl + T::ROWS;
+    float* stats = reinterpret_cast<float*>(lds + (AHEAD ? 4 : 2) * T::BYTES);        // per buffer: -lse (base 2) and D of the tile's rows
     const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if (logical >= total) return;
     const int per_head = key_tiles * nsplit, bh = logical / per_head, in = logical - bh * per_head, split = in / key_tiles, tile = in - split * key_tiles;
     const int b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
-    const AttnRows rows{a.Sq, G * a.Sq};
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-    const int len = key_count(a, b), key = tile * 128 + wave * 32 + (lane & 31);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, sub = wave >> 1;
+    const int len = key_count(a, b), key = tile * 64 + (wave & 1) * 32 + (lane & 31);
     const bool in_range = key < a.Skv, key_on = key < len && (!a.key_mask || a.key_mask[(long long)b * a.Skv + key] != 0);
-    float16_t adk[T::NV] = {}, adv[T::NV] = {};
+    // acc: dk, then dv.  What a lane whose key is not valid sums stays in its own column and is dropped at the end.
+    float16_t acc[2 * T::NV] = {};
     // a tile of keys that no query may look at has nothing to sum (uniform over the workgroup)
     if (__syncthreads_or(key_on)) {
+        const int head_tiles = (a.Sq + T::ROWS - 1) / T::ROWS, tiles = G * head_tiles;
+        const int t0 = (int)((long long)split * tiles / nsplit), t1 = (int)((long long)(split + 1) * tiles / nsplit);
+        int g = t0 / head_tiles, ht = t0 - g * head_tiles;                           // head and tile of the next fetch
+        using Stream = AttnStream<E, DP>;
+        const typename Stream::Map map(tid, a.D);
+        const unsigned char* qbase = static_cast<const unsigned char*>(a.q.p) + ((long long)b * a.q.b + (long long)(hk * G + g) * a.q.h) * T::ES;
+        const unsigned char* obase = static_cast<const unsigned char*>(a.dout.p) + ((long long)b * a.dout.b + (long long)(hk * G + g) * a.dout.h) * T::ES;
+        Stream sq(map, qbase, (long long)ht * T::ROWS, a.q.s), so(map, obase, (long long)ht * T::ROWS, a.dout.s);
+        float nlse = 0.f, dlt = 0.f;
+        auto fetch = [&] {
+            const int left = a.Sq - ht * T::ROWS;
+            const unsigned long long on = left >= T::ROWS ? ~0ull : (1ull << left) - 1;
+            sq.fetch(map, on);
+            so.fetch(map, on);
+            if (tid < T::ROWS) {
+                const long long at = ((long long)bh * G + g) * a.Sq + ht * T::ROWS + tid;
+                nlse = tid < left ? -a.lse[at] * kLog2e : -INFINITY;                 // a row behind the last: p = 0
+                dlt = tid < left ? parts.delta[at] : 0.f;
+            }
+            if (++ht == head_tiles) {
+                ht = 0;
+                ++g;
+                sq.jump(a.q.h * T::ES - head_tiles * sq.step);
+                so.jump(a.dout.h * T::ES - head_tiles * so.step);
+            }
+        };
+        if (AHEAD && t0 < t1) fetch();
         u32x4_t fk[T::KS], fv[T::KS];
         {
             const unsigned char* krow = static_cast<const unsigned char*>(a.k.p) + ((long long)b * a.k.b + (long long)hk * a.k.h + (long long)(key_on ? key : 0) * a.k.s) * T::ES;
@@ -145,56 +198,58 @@ template <typename E, int DP> __global__ void __launch_bounds__(256) attention_d
                 fv[ks] = load_channels<E>(vrow, (2 * ks + half) * T::V, key_on ? a.D : 0);
             }
         }
-        const int tiles = (rows.R + T::ROWS - 1) / T::ROWS;
-        const int t0 = (int)((long long)split * tiles / nsplit), t1 = (int)((long long)(split + 1) * tiles / nsplit);
         const float c2 = a.scale * kLog2e;
         for (int t = t0; t < t1; ++t) {
+            const int buffer = AHEAD ? (t - t0) & 1 : 0;
+            unsigned char* tq = lds + buffer * 2 * T::BYTES;
+            unsigned char* to = tq + T::BYTES;
+            float* tl = stats + buffer * 2 * T::ROWS;
+            float* td = tl + T::ROWS;
+            if (!AHEAD) {
+                fetch();
+                __syncthreads();
+            }
+            sq.put(map, tq);
+            so.put(map, to);
+            if (tid < T::ROWS) { tl[tid] = nlse; td[tid] = dlt; }
             __syncthreads();
+            if (AHEAD && t + 1 < t1) fetch();
+            float16_t s = {}, dp = {};
 #pragma unroll
-            for (int i = 0; i < T::LOADS; ++i) {
-                const int id = tid + 256 * i, qr = id / T::CPR, ch = id - qr * T::CPR;
-                if (qr < T::ROWS) {
-                    const int r = t * T::ROWS + qr;
-                    const bool ok = r < rows.R;
-                    *reinterpret_cast<u32x4_t*>(tq + T::at(qr, ch)) = load_channels<E>(ok ? rows.at(a.q, G, b, hk, r, T::ES) : nullptr, ch * T::V, ok ? a.D : 0);
-                    *reinterpret_cast<u32x4_t*>(to + T::at(qr, ch)) = load_channels<E>(ok ? rows.at(a.dout, G, b, hk, r, T::ES) : nullptr, ch * T::V, ok ? a.D : 0);
+            for (int ks = 0; ks < T::KS; ++ks) {
+                Mma<E>::run(T::along(tq, 32 * sub, ks, lane), fk[ks], s);
+                Mma<E>::run(T::along(to, 32 * sub, ks, lane), fv[ks], dp);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float4 nl = *reinterpret_cast<const float4*>(tl + 32 * sub + 8 * q + 4 * half), dl = *reinterpret_cast<const float4*>(td + 32 * sub + 8 * q + 4 * half);
+                const float n4[4] = {nl.x, nl.y, nl.z, nl.w}, d4[4] = {dl.x, dl.y, dl.z, dl.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * q + j], c2, n4[j]));
+                    s[4 * q + j] = p;
+                    dp[4 * q + j] = p * (dp[4 * q + j] - d4[j]);
                 }
             }
-            if (tid < T::ROWS) {
-                const int r = t * T::ROWS + tid;
-                const bool ok = r < rows.R;
-                tl[tid] = ok ? a.lse[(long long)bh * rows.R + r] * kLog2e : INFINITY;      // a row behind the last: p = 0
-                td[tid] = ok ? parts.delta[(long long)bh * rows.R + r] : 0.f;
-            }
-            __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float16_t s = {}, dp = {};
+            for (int st = 0; st < T::ST; ++st) {
+                const u32x4_t wp = T::weights(s, st), wd = T::weights(dp, st);
 #pragma unroll
-                for (int ks = 0; ks < T::KS; ++ks) {
-                    Mma<E>::run(T::along(tq, 32 * i, ks, lane), fk[ks], s);
-                    Mma<E>::run(T::along(to, 32 * i, ks, lane), fv[ks], dp);
-                }
-#pragma unroll
-                for (int q = 0; q < 16; ++q) {
-                    const int qr = 32 * i + 8 * (q / 4) + 4 * half + q % 4;
-                    const float p = key_on ? __builtin_amdgcn_exp2f(fmaf(s[q], c2, -tl[qr])) : 0.f;
-                    s[q] = p;
-                    dp[q] = key_on ? p * (dp[q] - td[qr]) : 0.f;
-                }
-#pragma unroll
-                for (int st = 0; st < T::ST; ++st) {
-                    const u32x4_t wp = T::weights(s, st), wd = T::weights(dp, st);
-#pragma unroll
-                    for (int d = 0; d < T::NV; ++d) {
-                        Mma<E>::run(T::across(to, 32 * i, st, d, lane), wp, adv[d]);
-                        Mma<E>::run(T::across(tq, 32 * i, st, d, lane), wd, adk[d]);
-                    }
+                for (int d = 0; d < T::NV; ++d) {
+                    Mma<E>::run(T::across(to, 32 * sub, st, d, lane), wp, acc[T::NV + d]);
+                    Mma<E>::run(T::across(tq, 32 * sub, st, d, lane), wd, acc[d]);
                 }
             }
         }
+        add_halves<2 * T::NV>(acc, lds, wave, lane);
     }
-    if (!in_range) return;
+    if (sub || !in_range) return;
+    if (!key_on) {
+#pragma unroll
+        for (int d = 0; d < 2 * T::NV; ++d)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[d][q] = 0.f;
+    }
     if (nsplit > 1) {
         const long long at = (((long long)split * a.B * a.Hkv + bh) * a.Skv + key) * a.D;
 #pragma unroll
@@ -203,8 +258,9 @@ template <typename E, int DP> __global__ void __launch_bounds__(256) attention_d
             for (int q = 0; q < 4; ++q) {
                 const int c = d * 32 + 8 * q + 4 * half;
                 if (c < a.D) {
-                    *reinterpret_cast<float4*>(parts.dk + at + c) = make_float4(adk[d][4 * q], adk[d][4 * q + 1], adk[d][4 * q + 2], adk[d][4 * q + 3]);
-                    *reinterpret_cast<float4*>(parts.dv + at + c) = make_float4(adv[d][4 * q], adv[d][4 * q + 1], adv[d][4 * q + 2], adv[d][4 * q + 3]);
+                    *reinterpret_cast<float4*>(parts.dk + at + c) = make_float4(acc[d][4 * q], acc[d][4 * q + 1], acc[d][4 * q + 2], acc[d][4 * q + 3]);
+                    *reinterpret_cast<float4*>(parts.dv + at + c) =
+                        make_float4(acc[T::NV + d][4 * q], acc[T::NV + d][4 * q + 1], acc[T::NV + d][4 * q + 2], acc[T::NV + d][4 * q + 3]);
                 }
             }
         return;
@@ -216,8 +272,8 @@ template <typename E, int DP> __global__ void __launch_bounds__(256) attention_d
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int c = d * 32 + 8 * q + 4 * half;
-            const float x[4] = {adk[d][4 * q] * a.scale, adk[d][4 * q + 1] * a.scale, adk[d][4 * q + 2] * a.scale, adk[d][4 * q + 3] * a.scale};
-            const float y[4] = {adv[d][4 * q], adv[d][4 * q + 1], adv[d][4 * q + 2], adv[d][4 * q + 3]};
+            const float x[4] = {acc[d][4 * q] * a.scale, acc[d][4 * q + 1] * a.scale, acc[d][4 * q + 2] * a.scale, acc[d][4 * q + 3] * a.scale};
+            const float y[4] = {acc[T::NV + d][4 * q], acc[T::NV + d][4 * q + 1], acc[T::NV + d][4 * q + 2], acc[T::NV + d][4 * q + 3]};
             store_channels<E>(dk, c, a.D, x);
             store_channels<E>(dv, c, a.D, y);
         }
@@ -247,8 +303,8 @@ template <typename E> __global__ void __launch_bounds__(256) attention_dkv_join_
 
 // Ranges of the query rows, where the keys alone leave compute units idle: about two workgroups a unit, at least four tiles of rows a range.
 int backward_ranges(int B, int Sq, int Skv, int H, int Hkv) {
-    const long long blocks = (long long)B * Hkv * (((long long)Skv + 127) / 128);
-    const long long tiles = ((long long)(H / Hkv) * Sq + 63) / 64;
+    const long long blocks = (long long)B * Hkv * (((long long)Skv + 63) / 64);
+    const long long tiles = (long long)(H / Hkv) * ((Sq + 63) / 64);
     long long n = 512 / blocks;
     if (n > tiles / 4) n = tiles / 4;
     if (n > 16) n = 16;
@@ -265,10 +321,10 @@ size_t attention_backward_ws_bytes(int B, int Sq, int Skv, int H, int Hkv, int D
 
 hipError_t launch_attention_backward(const AttnArgs& a, int dt, hipStream_t s) {
     const int R = a.H / a.Hkv * a.Sq, nsplit = backward_ranges(a.B, a.Sq, a.Skv, a.H, a.Hkv);
-    const int row_tiles = (R + 127) / 128, key_tiles = (a.Skv + 127) / 128;
+    const int row_tiles = (R + 63) / 64, key_tiles = (a.Skv + 63) / 64;
     const long long all = (long long)a.B * a.Hkv * R, qt = (long long)a.B * a.Hkv * row_tiles, kt = (long long)a.B * a.Hkv * key_tiles * nsplit;
     const long long joins = ((long long)a.B * a.Hkv * a.Skv * (a.D / 4) + 255) / 256;
-    if (qt > 0x3fffffffLL || kt > 0x3fffffffLL || (all + 15) / 16 > 0x7fffffffLL || joins > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (qt > 0x3fffffffLL || kt > 0x3fffffffLL || joins > 0x7fffffffLL) return hipErrorInvalidValue;
     BackwardParts parts{a.ws, nullptr, nullptr};
     if (nsplit > 1) {
         parts.dk = a.ws + align_floats((size_t)all);
@@ -276,26 +332,25 @@ hipError_t launch_attention_backward(const AttnArgs& a, int dt, hipStream_t s) {
     }
     return with_dtype(dt, [&](auto* tag) -> hipError_t {
         using E = std::remove_pointer_t<decltype(tag)>;
-        hipLaunchKernelGGL((attention_delta_kernel<E>), dim3((unsigned)((all + 15) / 16)), dim3(256), 0, s, a, parts.delta, all);
-        hipError_t rc = hipGetLastError();
-        if (rc != hipSuccess) return rc;
-        rc = with_channels(a.D, [&](auto dp) -> hipError_t {
+        const hipError_t rc = with_channels(a.D, [&](auto dp) -> hipError_t {
             constexpr int DP = decltype(dp)::value;
             if constexpr (sizeof(E) == 4 && DP > 10) return hipErrorInvalidValue;
             else {
                 using T = AttnTile<E, DP>;
-                constexpr int bytes = 2 * T::BYTES + 2 * T::ROWS * (int)sizeof(float);
-                static_assert(bytes <= 160 * 1024, "LDS budget");
+                constexpr int buffers = backward_ahead<E>() ? 2 : 1, halves = 2 * 1024 * T::NV * (int)sizeof(float);      // add_halves
+                constexpr int tiles_q = buffers * 2 * T::BYTES, tiles_k = tiles_q + buffers * 2 * T::ROWS * (int)sizeof(float);
+                constexpr int bytes_q = tiles_q > halves ? tiles_q : halves, bytes_k = tiles_k > 2 * halves ? tiles_k : 2 * halves;
+                static_assert(bytes_q <= 160 * 1024 && bytes_k <= 160 * 1024, "LDS budget");
                 auto kq = attention_dq_kernel<E, DP>;
                 auto kk = attention_dkv_kernel<E, DP>;
-                static const hipError_t attr_q = hipFuncSetAttribute(reinterpret_cast<const void*>(kq), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-                static const hipError_t attr_k = hipFuncSetAttribute(reinterpret_cast<const void*>(kk), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+                static const hipError_t attr_q = hipFuncSetAttribute(reinterpret_cast<const void*>(kq), hipFuncAttributeMaxDynamicSharedMemorySize, bytes_q);
+                static const hipError_t attr_k = hipFuncSetAttribute(reinterpret_cast<const void*>(kk), hipFuncAttributeMaxDynamicSharedMemorySize, bytes_k);
                 if (attr_q != hipSuccess || attr_k != hipSuccess) return hipErrorInvalidValue;
                 const int pq = (int)((qt + 7) / 8), pk = (int)((kt + 7) / 8);
-                hipLaunchKernelGGL(kq, dim3((unsigned)(pq * 8)), dim3(256), bytes, s, a, (const float*)parts.delta, row_tiles, (int)qt, pq);
+                hipLaunchKernelGGL(kq, dim3((unsigned)(pq * 8)), dim3(256), bytes_q, s, a, parts.delta, row_tiles, (int)qt, pq);
                 hipError_t e = hipGetLastError();
                 if (e != hipSuccess) return e;
-                hipLaunchKernelGGL(kk, dim3((unsigned)(pk * 8)), dim3(256), bytes, s, a, parts, key_tiles, nsplit, (int)kt, pk);
+                hipLaunchKernelGGL(kk, dim3((unsigned)(pk * 8)), dim3(256), bytes_k, s, a, parts, key_tiles, nsplit, (int)kt, pk);
                 return hipGetLastError();
             }
         });

@@ -84,6 +84,60 @@ template <typename E, int DP> struct AttnTile {
     }
 };
 
+// A thread's share (of 256) of the tiles of 64 rows that a workgroup streams: chunks of 16 bytes, on their way in registers until they are put into LDS.
+template <typename E, int DP> struct AttnStream {
+    using T = AttnTile<E, DP>;
+    static constexpr int N = T::LOADS;
+    static constexpr bool EVEN = T::ROWS * T::CPR % 256 == 0;   // every thread has N chunks
+    struct Map {                                                // where the chunks lie, the same for every tensor
+        int row[N], at[N], byte[N];
+        bool on[N];                                             // holds channels at all (a head's last chunk, and threads behind the tile's end, may not)
+        bool whole;                                             // uniform: all do
+        __device__ __forceinline__ Map(int tid, int D) {
+            whole = EVEN && D == DP * 16;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int id = tid + 256 * i, r = id / T::CPR, chunk = id - r * T::CPR;
+                on[i] = r < T::ROWS && chunk * T::V < D;
+                row[i] = r & 63;
+                byte[i] = chunk * 16;
+                at[i] = r < T::ROWS ? T::at(r, chunk) : -1;
+            }
+        }
+    };
+    u32x4_t f[N];
+    const unsigned char* p[N];
+    long long step;
+    // rows from `first` on of a tensor with `stride` elements between rows
+    __device__ __forceinline__ AttnStream(const Map& m, const unsigned char* base, long long first, long long stride) {
+        step = (long long)T::ROWS * stride * T::ES;
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = base + (first + m.row[i]) * stride * T::ES + m.byte[i];
+    }
+    // the next tile; rows whose bit is clear are zero and not read
+    __device__ __forceinline__ void fetch(const Map& m, unsigned long long rows) {
+        const u32x4_t zero = {0, 0, 0, 0};
+        if (m.whole && rows == ~0ull) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[i] = *reinterpret_cast<const u32x4_t*>(p[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[i] = m.on[i] && ((rows >> m.row[i]) & 1) ? *reinterpret_cast<const u32x4_t*>(p[i]) : zero;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] += step;
+    }
+    __device__ __forceinline__ void jump(long long bytes) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] += bytes;
+    }
+    __device__ __forceinline__ void put(const Map& m, unsigned char* tile) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (EVEN || m.at[i] >= 0) *reinterpret_cast<u32x4_t*>(tile + m.at[i]) = f[i];
+    }
+};
+
 // The rows that a key head's queries are dealt with as: r = g * Sq + s for query head hk * G + g, so that heads which share keys share a tile.
 struct AttnRows {
     int Sq, R;                       // R = G * Sq
