@@ -94,7 +94,7 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, const AttnParts& pa
 // 128 query rows per workgroup, 32 per wave; keys and values pass through LDS in tiles of 64 while the next tile is on its way in registers.
 // Two waves a SIMD as long as their registers suffice; wide heads give up the tile on its way for that.
 template <typename E, int DP> constexpr int attention_waves() { return DP <= (sizeof(E) == 2 ? 10 : 5) ? 2 : 1; }
-template <typename E, int DP> constexpr int attention_few_waves() { return DP <= (sizeof(E) == 2 ? 6 : 4) ? 2 : 1; }
+template <typename E, int DP> constexpr int attention_few_waves() { return DP <= 4 ? 2 : 1; }
 template <typename E, int DP> constexpr bool attention_ahead() { return sizeof(E) == 2 && DP <= 6; }
 template <typename E, int DP> __global__ void __launch_bounds__(256, (attention_waves<E, DP>()))
 attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int total, int per_xcd) {
@@ -102,7 +102,8 @@ attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int tot
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if (logical >= total) return;
-    const int per_head = row_tiles * nsplit, bh = logical / per_head, in = logical - bh * per_head, split = in / row_tiles, tile = in - split * row_tiles;
+    const int per_head = row_tiles * nsplit, slot = logical / per_head, in = logical - slot * per_head, split = in / row_tiles, tile = in - split * row_tiles;
+    const int bh = deal_heads(slot, a.B * a.Hkv);
     const int b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
     const AttnRows rows{a.Sq, G * a.Sq};
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
@@ -187,84 +188,113 @@ attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int tot
 }
 
 // At most 32 query rows a key head (one token of each query head that shares it, say): the four waves of a workgroup take different keys for the same
-// rows and are joined in LDS.  Bound by reading the keys: a wave's scores take them straight from memory, only the values, which the second
-// product needs across, pass through LDS of the wave's own; no barrier in the loop.
-template <typename E, int DP> __global__ void __launch_bounds__(256, (attention_few_waves<E, DP>()))
-attention_few_kernel(AttnArgs a, AttnParts parts, int nsplit, int total, int per_xcd) {
+// rows and are joined in LDS.  Bound by reading keys and values: each wave streams tiles of its own through LDS of its own, without a barrier in the loop,
+// with the next tile in flight (128 KB a compute unit at 128 channels).
+template <typename E, int DP> struct AttnFew {
     using T = AttnTile<E, DP>;
-    constexpr int KEYS = 32, WAVE_BYTES = KEYS * T::STRIDE, LOADS = (KEYS * T::CPR + 63) / 64;
+    static constexpr int SUBS = T::ES == 2 && DP <= 10 ? 2 : 1, KEYS = 32 * SUBS;
+    static constexpr int WAVE_BYTES = 2 * KEYS * T::STRIDE;    // keys, values
+    static constexpr int RPI = 64 / T::CPR;                    // rows that one load of the wave covers; the last lanes may have none
+    static constexpr int LOADS = (KEYS + RPI - 1) / RPI;
+    static constexpr int ROW = T::NV * 32 + 3;                 // floats per row and wave that are joined: channels, base, sum; odd
+    static constexpr int BYTES = 4 * (WAVE_BYTES > 32 * ROW * 4 ? WAVE_BYTES : 32 * ROW * 4);
+};
+template <typename E, int DP> __global__ void __launch_bounds__(256, (attention_few_waves<E, DP>()))
+attention_few_kernel(AttnArgs a, AttnParts parts, int nsplit) {
+    using T = AttnTile<E, DP>;
+    using F = AttnFew<E, DP>;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
-    if (logical >= total) return;
-    const int bh = logical / nsplit, split = logical - bh * nsplit;
+    const int bh = blockIdx.x / nsplit, split = blockIdx.x - bh * nsplit;       // no two workgroups read the same keys: no order among the XCDs
     const int b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
     const AttnRows rows{a.Sq, G * a.Sq};
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int r = lane & 31;
     const bool row_on = r < rows.R;
-    unsigned char* tv = lds + wave * WAVE_BYTES;
+    unsigned char* tk = lds + wave * F::WAVE_BYTES;
+    unsigned char* tv = tk + F::KEYS * T::STRIDE;
 
     const unsigned char* kbase = static_cast<const unsigned char*>(a.k.p) + ((long long)b * a.k.b + (long long)hk * a.k.h) * T::ES;
     const unsigned char* vbase = static_cast<const unsigned char*>(a.v.p) + ((long long)b * a.v.b + (long long)hk * a.v.h) * T::ES;
-    const int len = key_count(a, b), tiles = (len + KEYS - 1) / KEYS, part = split * 4 + wave;
+    const int len = key_count(a, b), tiles = (len + F::KEYS - 1) / F::KEYS, part = split * 4 + wave;
     const int t0 = (int)((long long)part * tiles / (nsplit * 4)), t1 = (int)((long long)(part + 1) * tiles / (nsplit * 4));
-    u32x4_t fq[T::KS], fk[T::KS], lv[LOADS];
+    // this lane's chunk of each load: a 32-bit offset behind a wave-uniform place (the launcher checks the strides for that)
+    const int lrow = lane / T::CPR, chunk = lane - lrow * T::CPR;
+    const bool lane_on = lrow < F::RPI && chunk * T::V < a.D, whole = a.D == DP * 16 && 64 % T::CPR == 0;
+    const uint32_t koff = (uint32_t)(lrow * a.k.s * T::ES) + chunk * 16, voff = (uint32_t)(lrow * a.v.s * T::ES) + chunk * 16;
+    u32x4_t fq[T::KS], lk[F::LOADS], lv[F::LOADS];
+    const u32x4_t zero = {0, 0, 0, 0};
+    constexpr unsigned long long ALL = F::SUBS == 2 ? ~0ull : 0xffffffffull;
+    auto mask = [&](int t) { return valid_keys(a, b, t * F::KEYS, len) & ALL; };
+    auto fetch = [&](int t, unsigned long long on) {
+        const unsigned char* kt = kbase + (long long)t * F::KEYS * a.k.s * T::ES;
+        const unsigned char* vt = vbase + (long long)t * F::KEYS * a.v.s * T::ES;
+        const long long kstep = F::RPI * a.k.s * T::ES, vstep = F::RPI * a.v.s * T::ES;
+        if (whole && on == ALL) {
+#pragma unroll
+            for (int i = 0; i < F::LOADS; ++i) lk[i] = *reinterpret_cast<const u32x4_t*>(kt + i * kstep + koff);
+#pragma unroll
+            for (int i = 0; i < F::LOADS; ++i) lv[i] = *reinterpret_cast<const u32x4_t*>(vt + i * vstep + voff);
+        } else {
+#pragma unroll
+            for (int i = 0; i < F::LOADS; ++i) {
+                const int row = i * F::RPI + lrow;
+                const bool ok = lane_on && row < F::KEYS && ((on >> (row & 63)) & 1);
+                lk[i] = ok ? *reinterpret_cast<const u32x4_t*>(kt + i * kstep + koff) : zero;
+                lv[i] = ok ? *reinterpret_cast<const u32x4_t*>(vt + i * vstep + voff) : zero;
+            }
+        }
+    };
+    auto put = [&] {
+#pragma unroll
+        for (int i = 0; i < F::LOADS; ++i) {
+            const int row = i * F::RPI + lrow, at = T::at(row, chunk);
+            if (64 % T::CPR == 0 || (lrow < F::RPI && row < F::KEYS)) {
+                *reinterpret_cast<u32x4_t*>(tk + at) = lk[i];
+                *reinterpret_cast<u32x4_t*>(tv + at) = lv[i];
+            }
+        }
+    };
+    unsigned long long on = t0 < t1 ? mask(t0) : 0;
+    if (t0 < t1) fetch(t0, on);
     {
         const unsigned char* qrow = row_on ? rows.at(a.q, G, b, hk, r, T::ES) : nullptr;
 #pragma unroll
         for (int ks = 0; ks < T::KS; ++ks) fq[ks] = load_channels<E>(qrow, (2 * ks + half) * T::V, row_on ? a.D : 0);
     }
-    auto mask = [&](int t) { return valid_keys(a, b, t * KEYS, len) & 0xffffffffull; };
-    auto fetch_keys = [&](int t, unsigned long long on) {
-        const bool ok = (on >> r) & 1;
-        const unsigned char* row = kbase + ((long long)t * KEYS + r) * a.k.s * T::ES;
-#pragma unroll
-        for (int ks = 0; ks < T::KS; ++ks) fk[ks] = load_channels<E>(row, (2 * ks + half) * T::V, ok ? a.D : 0);
-    };
-    auto fetch_values = [&](int t, unsigned long long on) {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int id = lane + 64 * i, row = id / T::CPR, c = (id - row * T::CPR) * T::V;
-            const bool ok = row < KEYS && ((on >> (row & 31)) & 1);
-            lv[i] = load_channels<E>(vbase + ((long long)t * KEYS + row) * a.v.s * T::ES, c, ok ? a.D : 0);
-        }
-    };
     AttnState<E, DP> st;
     const float c2 = a.scale * kLog2e;
-    unsigned long long on = t0 < t1 ? mask(t0) : 0;
-    if (t0 < t1) { fetch_keys(t0, on); fetch_values(t0, on); }
     for (int t = t0; t < t1; ++t) {
         const unsigned long long cur = on;
-        float16_t s[1] = {};
-#pragma unroll
-        for (int ks = 0; ks < T::KS; ++ks) Mma<E>::run(fk[ks], fq[ks], s[0]);
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int id = lane + 64 * i, row = id / T::CPR;
-            if (row < KEYS) *reinterpret_cast<u32x4_t*>(tv + T::at(row, id - row * T::CPR)) = lv[i];
-        }
+        __builtin_amdgcn_wave_barrier();                   // a tile in LDS is written and read by this wave alone, in order
+        put();
+        __builtin_amdgcn_wave_barrier();
         if (t + 1 < t1) {
             on = mask(t + 1);
-            fetch_keys(t + 1, on);
-            fetch_values(t + 1, on);
+            fetch(t + 1, on);
         }
         if (cur == 0) continue;                            // uniform over the wave
-        st.template settle<1>(s, cur, half, c2);
-        st.weigh(s[0], c2, st.shift());
-        __builtin_amdgcn_wave_barrier();                   // the values of this tile are in LDS: written and read by this wave, in order
+        float16_t s[F::SUBS] = {};
 #pragma unroll
-        for (int k = 0; k < T::ST; ++k) {
-            const u32x4_t w = T::weights(s[0], k);
+        for (int i = 0; i < F::SUBS; ++i)
 #pragma unroll
-            for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(tv, 0, k, d, lane), w, st.acc[d]);
+            for (int ks = 0; ks < T::KS; ++ks) Mma<E>::run(T::along(tk, 32 * i, ks, lane), fq[ks], s[i]);
+        st.template settle<F::SUBS>(s, cur, half, c2);
+        const float sh = st.shift();
+#pragma unroll
+        for (int i = 0; i < F::SUBS; ++i) {
+            st.weigh(s[i], c2, sh);
+#pragma unroll
+            for (int k = 0; k < T::ST; ++k) {
+                const u32x4_t w = T::weights(s[i], k);
+#pragma unroll
+                for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(tv, 32 * i, k, d, lane), w, st.acc[d]);
+            }
         }
-        __builtin_amdgcn_wave_barrier();
     }
     // join the four waves: each leaves base, sum and channels; wave 0 adds them up in order
     st.l += __shfl_xor(st.l, 32);
     __syncthreads();
-    constexpr int ROW = T::NV * 32 + 2;                    // floats per row and wave: channels, base, sum
-    float* mine = reinterpret_cast<float*>(lds) + (wave * 32 + r) * (ROW + 1);
+    float* mine = reinterpret_cast<float*>(lds) + (wave * 32 + r) * F::ROW;
     if (row_on) {
 #pragma unroll
         for (int d = 0; d < T::NV; ++d)
@@ -274,8 +304,8 @@ attention_few_kernel(AttnArgs a, AttnParts parts, int nsplit, int total, int per
     }
     __syncthreads();
     if (wave != 0 || !row_on) return;
-    const float* all = reinterpret_cast<const float*>(lds) + r * (ROW + 1);
-    constexpr int STEP = 32 * (ROW + 1);
+    const float* all = reinterpret_cast<const float*>(lds) + r * F::ROW;
+    constexpr int STEP = 32 * F::ROW;
     float base = -INFINITY;
 #pragma unroll
     for (int w = 0; w < 4; ++w) base = fmaxf(base, all[w * STEP + T::NV * 32]);
@@ -300,26 +330,46 @@ attention_few_kernel(AttnArgs a, AttnParts parts, int nsplit, int total, int per
     store_row<E, DP>(a, parts, rows, G, b, hk, r, split, nsplit, half, st, inv, lse2);
 }
 
-// one wave per row: the ranges' results, weighted by their sums
+// one workgroup per row: the ranges' results, weighted by their sums (lane i has range i's; there are at most 64).  What it reads was written by other
+// XCDs a moment ago and is 2 us away: wave w takes ranges w, w + 4, ..., and everything is requested before the first weight is known.
 template <typename E> __global__ void __launch_bounds__(256) attention_join_kernel(AttnArgs a, AttnParts parts, int nsplit, long long all) {
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= all) return;
-    const int lane = threadIdx.x & 63, G = a.H / a.Hkv;
+    const long long row = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = a.H / a.Hkv;
     const AttnRows rows{a.Sq, G * a.Sq};
-    float m = -INFINITY;
-    for (int i = 0; i < nsplit; ++i) m = fmaxf(m, parts.lse2[i * all + row]);
-    const float base = m == -INFINITY ? 0.f : m;
-    float total = 0.f;
-    for (int i = 0; i < nsplit; ++i) total += __builtin_amdgcn_exp2f(parts.lse2[i * all + row] - base);
-    const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
-    const int bh = (int)(row / rows.R), r = (int)(row - (long long)bh * rows.R), b = bh / a.Hkv, hk = bh - b * a.Hkv;
+    __shared__ float sums[4][256];
+    const float lse2 = lane < nsplit ? parts.lse2[lane * all + row] : -INFINITY;
+    float v[4] = {}, first[4][4];
+    const float* base = parts.o + row * a.D;
+    const long long step = all * a.D;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) first[i][c] = wave + 4 * i < nsplit && lane + 64 * c < a.D ? base[(wave + 4 * i) * step + lane + 64 * c] : 0.f;
+    float m = lse2;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    float w = __builtin_amdgcn_exp2f(lse2 - (m == -INFINITY ? 0.f : m)), total = w;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+    w *= total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
+    auto weight = [&](int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i)); };
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (wave + 4 * i < nsplit) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = fmaf(weight(wave + 4 * i), first[i][c], v[c]);
+        }
+    for (int i = wave + 16; i < nsplit; i += 4)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (lane + 64 * c < a.D) v[c] = fmaf(weight(i), base[i * step + lane + 64 * c], v[c]);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) sums[wave][lane + 64 * c] = v[c];
+    __syncthreads();
+    const int bh = (int)(row / rows.R), r = (int)(row - (long long)bh * rows.R), b = bh / a.Hkv, hk = bh - b * a.Hkv, c = threadIdx.x;
     E* o = reinterpret_cast<E*>(const_cast<unsigned char*>(rows.at(a.o, G, b, hk, r, (int)sizeof(E))));
-    for (int c = lane; c < a.D; c += 64) {
-        float v = 0.f;
-        for (int i = 0; i < nsplit; ++i) v = fmaf(__builtin_amdgcn_exp2f(parts.lse2[i * all + row] - base) * inv, parts.o[(i * all + row) * a.D + c], v);
-        o[c] = from_f32<E>(v);
-    }
-    if (a.lse && lane == 0) a.lse[row] = total == 0.f ? -INFINITY : (m + log2f(total)) * kLn2;
+    if (c < a.D) o[c] = from_f32<E>((sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]));
+    if (a.lse && threadIdx.x == 0) a.lse[row] = total == 0.f ? -INFINITY : (m + log2f(total)) * kLn2;
 }
 
 // Whether the rows of a key head fit one wave's tile.
@@ -347,7 +397,7 @@ size_t attention_ws_bytes(int B, int Sq, int Skv, int H, int Hkv, int D, int) {
 hipError_t launch_attention(const AttnArgs& a, int dt, hipStream_t s) {
     const int R = a.H / a.Hkv * a.Sq, nsplit = attention_ranges(a.B, a.Sq, a.Skv, a.H, a.Hkv), row_tiles = (R + 127) / 128;
     const long long all = (long long)a.B * a.Hkv * R, total = (long long)a.B * a.Hkv * row_tiles * nsplit;
-    if (total > 0x3fffffffLL || (all + 3) / 4 > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (total > 0x3fffffffLL || all > 0x7fffffffLL) return hipErrorInvalidValue;
     const int per_xcd = (int)((total + 7) / 8);
     AttnParts parts{nullptr, nullptr};
     if (nsplit > 1) { parts.o = a.ws; parts.lse2 = a.ws + (size_t)nsplit * all * a.D; }
@@ -358,15 +408,16 @@ hipError_t launch_attention(const AttnArgs& a, int dt, hipStream_t s) {
             if constexpr (sizeof(E) == 4 && DP > 10) return hipErrorInvalidValue;
             else {
                 using T = AttnTile<E, DP>;
-                if (few_rows(a.Sq, a.H, a.Hkv)) {
-                    auto kern = attention_few_kernel<E, DP>;
-                    constexpr int tiles = 4 * 32 * T::STRIDE, joined = 4 * 32 * (T::NV * 32 + 3) * 4, bytes = tiles > joined ? tiles : joined;
-                    static_assert(bytes <= 160 * 1024, "LDS budget");
-                    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-                    if (attr != hipSuccess) return attr;
-                    const int count = a.B * a.Hkv * nsplit, each = (count + 7) / 8;
-                    hipLaunchKernelGGL(kern, dim3((unsigned)(each * 8)), dim3(256), bytes, s, a, parts, nsplit, count, each);
-                    return hipGetLastError();
+                if constexpr (AttnFew<E, DP>::BYTES <= 160 * 1024) {           // fp32 with more than 128 channels does not fit
+                    // (offsets within a load of the few-rows kernel are 32 bits wide)
+                    if (few_rows(a.Sq, a.H, a.Hkv) && (a.k.s | a.v.s) < (1LL << 24)) {
+                        auto kern = attention_few_kernel<E, DP>;
+                        constexpr int bytes = AttnFew<E, DP>::BYTES;
+                        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+                        if (attr != hipSuccess) return attr;
+                        hipLaunchKernelGGL(kern, dim3((unsigned)(a.B * a.Hkv * nsplit)), dim3(256), bytes, s, a, parts, nsplit);
+                        return hipGetLastError();
+                    }
                 }
                 auto kern = attention_kernel<E, DP>;
                 constexpr int bytes = (attention_ahead<E, DP>() ? 4 : 2) * T::BYTES;
@@ -378,7 +429,7 @@ hipError_t launch_attention(const AttnArgs& a, int dt, hipStream_t s) {
             }
         });
         if (rc != hipSuccess || nsplit == 1) return rc;
-        hipLaunchKernelGGL((attention_join_kernel<E>), dim3((unsigned)((all + 3) / 4)), dim3(256), 0, s, a, parts, nsplit, all);
+        hipLaunchKernelGGL((attention_join_kernel<E>), dim3((unsigned)all), dim3(256), 0, s, a, parts, nsplit, all);
         return hipGetLastError();
     });
 }

@@ -47,7 +47,7 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if (logical >= total) return;
-    const int bh = logical / row_tiles, tile = logical - bh * row_tiles, b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
+    const int slot = logical / row_tiles, tile = logical - slot * row_tiles, bh = deal_heads(slot, a.B * a.Hkv), b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
     const AttnRows rows{a.Sq, G * a.Sq};
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, sub = wave >> 1;
     const int r = tile * 64 + (wave & 1) * 32 + (lane & 31);
@@ -152,7 +152,8 @@ attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit,
     float* stats = reinterpret_cast<float*>(lds + (AHEAD ? 4 : 2) * T::BYTES);        // per buffer: -lse (base 2) and D of the tile's rows
     const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if (logical >= total) return;
-    const int per_head = key_tiles * nsplit, bh = logical / per_head, in = logical - bh * per_head, split = in / key_tiles, tile = in - split * key_tiles;
+    const int per_head = key_tiles * nsplit, slot = logical / per_head, in = logical - slot * per_head, split = in / key_tiles, tile = in - split * key_tiles;
+    const int bh = deal_heads(slot, a.B * a.Hkv);
     const int b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, sub = wave >> 1;
     const int len = key_count(a, b), key = tile * 64 + (wave & 1) * 32 + (lane & 31);

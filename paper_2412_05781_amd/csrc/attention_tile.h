@@ -173,6 +173,12 @@ __device__ __forceinline__ int key_count(const AttnArgs& a, int b) {
     return n < 0 ? 0 : n < a.Skv ? n : a.Skv;
 }
 
+// Each XCD runs a contiguous range of the workgroups' order, whole heads after one another, so that a head's streamed rows stay in one L2.  Lengths differ
+// between the batch's rows, not between heads: where the heads divide evenly, neighbours go to different XCDs.
+__device__ __forceinline__ int deal_heads(int bh, int heads) {
+    return heads % 8 ? bh : (bh % (heads / 8)) * 8 + bh / (heads / 8);
+}
+
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 
 // channels / 16 as a compile-time number
