@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -151,7 +152,7 @@ def lib() -> ctypes.CDLL:
             f = getattr(L, f"wino_{name}_workspace_bytes")
             f.restype = sz; f.argtypes = [i] * 7
             f = getattr(L, f"wino_{name}")
-            f.restype = i; f.argtypes = [ctypes.POINTER(wino_attention_args), vp, sz, vp]
+            f.restype = i; f.argtypes = [vp, vp, sz, vp]           # the struct by reference, or packed as bytes
         _lib = L
     return _lib
 
@@ -634,6 +635,8 @@ def wino_i8_batched_gemm(Uq: torch.Tensor, dU: torch.Tensor, Vq: torch.Tensor, d
 
 
 # ---- operators of a transformer block -----------------------------------------------------------
+# The smallest of these calls are one kernel of a few microseconds: shapes and strides are asked for once each, and the attention call's argument struct is
+# packed in one go (field by field through ctypes it costs as much as the launch).
 def _on_one_device(stream, first, *others):
     """Every tensor lives on `first`'s GPU, and that is the current one unless a stream is named (kernels go where the stream is)."""
     d = first.get_device()
@@ -646,23 +649,24 @@ def _on_one_device(stream, first, *others):
         raise ValueError(f"tensors live on GPU {d}, which is not the one the call runs on")
 
 
-def _rows(t: torch.Tensor, name: str, rows: int, cols: int, dtype) -> int:
+def _rows(t: torch.Tensor, name: str, shape, dtype) -> int:
     """The row stride of a [rows, cols] tensor whose rows are contiguous."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype != dtype:
-        raise ValueError(f"{name} must be [{rows}, {cols}] of {dtype}")
-    if cols > 1 and t.stride(1) != 1:
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must be {list(shape)} of {dtype}")
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return t.stride(0) if rows > 1 else cols
+    return ld if shape[0] > 1 else shape[1]
 
 
 def _weights(x, w, bias, halves: int):
-    """(M, N, K, dtype code) of x[M,K], w[halves*N,K] and bias[halves*N]."""
-    dt = DTYPE_OF.get(x.dtype)
-    if dt is None or x.dim() != 2 or w.dim() != 2 or w.dtype != x.dtype or w.shape[1] != x.shape[1] or w.shape[0] % halves or not w.is_contiguous():
+    """(x's shape, N, dtype code) of x[M,K], w[halves*N,K] and bias[halves*N]."""
+    dt, xs, ws = DTYPE_OF.get(x.dtype), x.shape, w.shape
+    if dt is None or len(xs) != 2 or len(ws) != 2 or w.dtype != x.dtype or ws[1] != xs[1] or ws[0] % halves or not w.is_contiguous():
         raise ValueError("x must be [M, K] and w a contiguous [N, K] (gated: [2N, K]) of the same storage type")
-    if bias is not None and (bias.dtype != torch.float32 or bias.numel() != w.shape[0] or not bias.is_contiguous()):
+    if bias is not None and (bias.dtype != torch.float32 or bias.numel() != ws[0] or not bias.is_contiguous()):
         raise ValueError("bias must be a contiguous fp32 tensor with one element per row of w")
-    return x.shape[0], w.shape[0] // halves, x.shape[1], dt
+    return xs, ws[0] // halves, dt
 
 
 def _ws(workspace):
@@ -691,9 +695,10 @@ def wino_glu_backward_workspace_bytes(M, N, K, dtype, act) -> int:
 
 def wino_linear(x, w, bias, y, act: int = WINO_ACT_NONE, residual=None, workspace=None, stream=None):
     """y[M,N] = act(x[M,K] w[N,K]^T + bias) + residual; rows of x, y and residual may be strided, residual may be y."""
-    M, N, K, dt = _weights(x, w, bias, 1)
-    ldx, ldy = _rows(x, "x", M, K, x.dtype), _rows(y, "y", M, N, x.dtype)
-    ldr = ldy if residual is None else _rows(residual, "residual", M, N, x.dtype)
+    xs, N, dt = _weights(x, w, bias, 1)
+    M, K = xs
+    ldx, ldy = _rows(x, "x", xs, x.dtype), _rows(y, "y", (M, N), x.dtype)
+    ldr = ldy if residual is None else _rows(residual, "residual", (M, N), x.dtype)
     _on_one_device(stream, x, w, bias, y, residual, workspace)
     ws, n = _ws(workspace)
     _check(lib().wino_linear(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), y.data_ptr(), M, N, K, ldx, ldr, ldy, dt, act, ws, n,
@@ -702,9 +707,10 @@ def wino_linear(x, w, bias, y, act: int = WINO_ACT_NONE, residual=None, workspac
 
 
 def _product_backward(name, halves, x, w, bias, dy, dx, dw, dbias, act, workspace, stream):
-    M, N, K, dt = _weights(x, w, bias, halves)
-    ldx, lddy = _rows(x, "x", M, K, x.dtype), _rows(dy, "the output's gradient", M, N, x.dtype)
-    lddx = K if dx is None else _rows(dx, "dx", M, K, x.dtype)
+    xs, N, dt = _weights(x, w, bias, halves)
+    M, K = xs
+    ldx, lddy = _rows(x, "x", xs, x.dtype), _rows(dy, "the output's gradient", (M, N), x.dtype)
+    lddx = K if dx is None else _rows(dx, "dx", xs, x.dtype)
     if dw is not None and (dw.shape != w.shape or dw.dtype != x.dtype or not dw.is_contiguous()):
         raise ValueError("dw must be contiguous with the shape and type of w")
     if dbias is not None and (dbias.dtype != torch.float32 or dbias.numel() != halves * N or not dbias.is_contiguous()):
@@ -723,8 +729,9 @@ def wino_linear_backward(x, w, bias, dy, dx, dw, dbias, act: int = WINO_ACT_NONE
 
 def wino_glu(x, w, bias, h, act: int = WINO_ACT_GELU, workspace=None, stream=None):
     """h[M,N] = (x wu^T + bu) * act(x wg^T + bg) with w[2N,K] = wu above wg and bias[2N] = bu, bg."""
-    M, N, K, dt = _weights(x, w, bias, 2)
-    ldx, ldh = _rows(x, "x", M, K, x.dtype), _rows(h, "h", M, N, x.dtype)
+    xs, N, dt = _weights(x, w, bias, 2)
+    M, K = xs
+    ldx, ldh = _rows(x, "x", xs, x.dtype), _rows(h, "h", (M, N), x.dtype)
     _on_one_device(stream, x, w, bias, h, workspace)
     ws, n = _ws(workspace)
     _check(lib().wino_glu(x.data_ptr(), w.data_ptr(), _ptr(bias), h.data_ptr(), M, N, K, ldx, ldh, dt, act, ws, n, _stream(stream)), "wino_glu")
@@ -744,36 +751,39 @@ def wino_attention_backward_workspace_bytes(B, Sq, Skv, H, Hkv, D, dtype) -> int
     return lib().wino_attention_backward_workspace_bytes(B, Sq, Skv, H, Hkv, D, dtype)
 
 
-def _heads(field, t, name, shape, dtype):
-    if t.shape != shape or t.dtype != dtype or (t.stride(3) != 1 and shape[3] > 1):
+def _heads(t, name, shape, dtype):
+    """(address, strides of batch, position and head): a wino_tensor"""
+    st = t.stride()
+    if t.shape != shape or t.dtype != dtype or (st[-1] != 1 and shape[3] > 1):
         raise ValueError(f"{name} must be {list(shape)} of {dtype} with contiguous channels")
-    field.data = t.data_ptr()
-    field.stride_b, field.stride_s, field.stride_h, _ = t.stride()
+    return t.data_ptr(), *st[:3]
 
 
-def _attention(q, k, v, o, lse, kv_len, key_mask, scale):
-    if q.dim() != 4 or k.dim() != 4 or q.dtype not in DTYPE_OF:
+_ATTENTION_ARGS = struct.Struct("@7if" + "Pqqq" * 4 + "PPP" + "Pqqq" * 4)        # wino_attention_args
+_NO_GRADIENTS = (0,) * 16
+
+
+def _attention(q, k, v, o, lse, kv_len, key_mask, scale, gradients=None):
+    qs, ks, dtype = q.shape, k.shape, q.dtype
+    if len(qs) != 4 or len(ks) != 4 or dtype not in DTYPE_OF:
         raise ValueError("q must be [B, Sq, H, D] and k, v [B, Skv, Hkv, D] in one of the storage types")
-    B, Sq, H, D = q.shape
-    _, Skv, Hkv, _ = kshape = k.shape
-    a = wino_attention_args(B, Sq, Skv, H, Hkv, D, DTYPE_OF[q.dtype], D ** -0.5 if scale is None else scale)
-    _heads(a.q, q, "q", q.shape, q.dtype)
-    _heads(a.k, k, "k", (B, Skv, Hkv, D), q.dtype)
-    _heads(a.v, v, "v", kshape, q.dtype)
-    _heads(a.o, o, "o", q.shape, q.dtype)
-    if lse is not None:
-        if lse.dtype != torch.float32 or lse.shape != (B, H, Sq) or not lse.is_contiguous():
-            raise ValueError("lse must be a contiguous fp32 tensor [B, H, Sq]")
-        a.lse = lse.data_ptr()
-    if kv_len is not None:
-        if kv_len.dtype != torch.int32 or kv_len.shape != (B,) or not kv_len.is_contiguous():
-            raise ValueError("kv_len must be a contiguous int32 tensor [B]")
-        a.kv_len = kv_len.data_ptr()
-    if key_mask is not None:
-        if key_mask.dtype not in (torch.uint8, torch.bool) or key_mask.shape != (B, Skv) or not key_mask.is_contiguous():
-            raise ValueError("key_mask must be a contiguous uint8 or bool tensor [B, Skv]")
-        a.key_mask = key_mask.data_ptr()
-    return a
+    B, Sq, H, D = qs
+    Skv, Hkv = ks[1], ks[2]
+    ks = (B, Skv, Hkv, D)
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, H, Sq) or not lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous fp32 tensor [B, H, Sq]")
+    if kv_len is not None and (kv_len.dtype != torch.int32 or kv_len.shape != (B,) or not kv_len.is_contiguous()):
+        raise ValueError("kv_len must be a contiguous int32 tensor [B]")
+    if key_mask is not None and (key_mask.dtype not in (torch.uint8, torch.bool) or key_mask.shape != (B, Skv) or not key_mask.is_contiguous()):
+        raise ValueError("key_mask must be a contiguous uint8 or bool tensor [B, Skv]")
+    if gradients is None:
+        g = _NO_GRADIENTS
+    else:
+        do, dq, dk, dv = gradients
+        g = (*_heads(do, "do", qs, dtype), *_heads(dq, "dq", qs, dtype), *_heads(dk, "dk", ks, dtype), *_heads(dv, "dv", ks, dtype))
+    return _ATTENTION_ARGS.pack(B, Sq, Skv, H, Hkv, D, DTYPE_OF[dtype], D ** -0.5 if scale is None else scale, *_heads(q, "q", qs, dtype),
+                                *_heads(k, "k", ks, dtype), *_heads(v, "v", ks, dtype), *_heads(o, "o", qs, dtype), _ptr(lse) or 0, _ptr(kv_len) or 0,
+                                _ptr(key_mask) or 0, *g)
 
 
 def wino_attention(q, k, v, o, lse=None, kv_len=None, key_mask=None, scale=None, workspace=None, stream=None):
@@ -782,20 +792,16 @@ def wino_attention(q, k, v, o, lse=None, kv_len=None, key_mask=None, scale=None,
     a = _attention(q, k, v, o, lse, kv_len, key_mask, scale)
     _on_one_device(stream, q, k, v, o, lse, kv_len, key_mask, workspace)
     ws, n = _ws(workspace)
-    _check(lib().wino_attention(ctypes.byref(a), ws, n, _stream(stream)), "wino_attention")
+    _check(lib().wino_attention(a, ws, n, _stream(stream)), "wino_attention")
     return o
 
 
 def wino_attention_backward(q, k, v, o, lse, do, dq, dk, dv, kv_len=None, key_mask=None, scale=None, workspace=None, stream=None):
     """Gradients of q, k and v for do, from the inputs and results (o, lse) of wino_attention."""
-    a = _attention(q, k, v, o, lse, kv_len, key_mask, scale)
-    _heads(a.d_o, do, "do", q.shape, q.dtype)
-    _heads(a.dq, dq, "dq", q.shape, q.dtype)
-    _heads(a.dk, dk, "dk", k.shape, q.dtype)
-    _heads(a.dv, dv, "dv", k.shape, q.dtype)
+    a = _attention(q, k, v, o, lse, kv_len, key_mask, scale, (do, dq, dk, dv))
     _on_one_device(stream, q, k, v, o, lse, do, dq, dk, dv, kv_len, key_mask, workspace)
     ws, n = _ws(workspace)
-    _check(lib().wino_attention_backward(ctypes.byref(a), ws, n, _stream(stream)), "wino_attention_backward")
+    _check(lib().wino_attention_backward(a, ws, n, _stream(stream)), "wino_attention_backward")
     return dq, dk, dv
 
 

@@ -181,7 +181,7 @@ extern "C" {
 
 size_t wino_linear_workspace_bytes(int M, int N, int K, int dtype, int act) {
     if (!is_dtype(dtype) || !is_act(act) || !product_dims_ok(M, N, K, 1)) return 0;
-    return product_bytes(M, N, K, dtype);
+    return few_gemm_ok(M) ? 0 : product_bytes(M, N, K, dtype);
 }
 
 int wino_linear(const void* x, const void* w, const float* bias, const void* residual, void* y, int M, int N, int K, long long ldx, long long ldr,
@@ -194,13 +194,16 @@ int wino_linear(const void* x, const void* w, const float* bias, const void* res
     const size_t es = bytes_of(dtype), ny = extent(M, ldy, N, es);
     if (overlap(y, ny, x, extent(M, ldx, K, es)) || overlap(y, ny, w, (size_t)N * K * es) || overlap(y, ny, bias, (size_t)N * 4)) return WINO_ERR_ALIAS;
     if (residual && !(residual == y && ldr == ldy) && overlap(y, ny, residual, extent(M, ldr, N, es))) return WINO_ERR_ALIAS;
-    const size_t need = product_bytes(M, N, K, dtype);
+    const size_t need = few_gemm_ok(M) ? 0 : product_bytes(M, N, K, dtype);
     if (need && (!workspace || workspace_bytes < need)) return WINO_ERR_WORKSPACE;
     if (need && !at16(workspace)) return WINO_ERR_ALIGN;
     Epilogue e;
     e.bias = bias; e.extra = residual; e.ld_extra = ldr; e.out = y; e.ld_out = ldy; e.act = act;
-    return product(EP_LINEAR, false, false, Operand{w, K}, Operand{x, ldx}, GemmShape{M, N, K}, e, workspace, dtype, static_cast<hipStream_t>(stream)) == hipSuccess
-               ? WINO_OK : WINO_ERR_HIP;
+    const Operand P{w, K}, Q{x, ldx};
+    const GemmShape g{M, N, K};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const hipError_t rc = few_gemm_ok(M) ? launch_few_gemm(false, P, Q, g, e, dtype, s) : product(EP_LINEAR, false, false, P, Q, g, e, workspace, dtype, s);
+    return rc == hipSuccess ? WINO_OK : WINO_ERR_HIP;
 }
 
 size_t wino_linear_backward_workspace_bytes(int M, int N, int K, int dtype, int act) {
@@ -227,8 +230,11 @@ int wino_glu(const void* x, const void* w, const float* bias, void* h, int M, in
     if (overlap(h, nh, x, extent(M, ldx, K, es)) || overlap(h, nh, w, 2 * (size_t)N * K * es) || overlap(h, nh, bias, 2 * (size_t)N * 4)) return WINO_ERR_ALIAS;
     Epilogue e;
     e.bias = bias; e.out = h; e.ld_out = ldh; e.act = act;
-    return launch_gemm(EP_GLU, false, false, Operand{w, K}, Operand{x, ldx}, GemmShape{M, N, K}, e, 1, dtype, static_cast<hipStream_t>(stream)) == hipSuccess
-               ? WINO_OK : WINO_ERR_HIP;
+    const Operand P{w, K}, Q{x, ldx};
+    const GemmShape g{M, N, K};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const hipError_t rc = few_gemm_ok(M) ? launch_few_gemm(true, P, Q, g, e, dtype, s) : launch_gemm(EP_GLU, false, false, P, Q, g, e, 1, dtype, s);
+    return rc == hipSuccess ? WINO_OK : WINO_ERR_HIP;
 }
 
 size_t wino_glu_backward_workspace_bytes(int M, int N, int K, int dtype, int act) {

@@ -46,6 +46,9 @@ int gemm_most_sum_rows(int M);
 int gemm_ranges(int M, int N, int K, int dt);
 hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit,
                        int dt, hipStream_t s, int* sum_rows = nullptr);
+// x W^T with EP_LINEAR or (glu) EP_GLU for few rows, one kernel, no workspace
+bool few_gemm_ok(int M);
+hipError_t launch_few_gemm(bool glu, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s);
 // out = act(sum over ranges + bias) + extra
 hipError_t launch_join(const float* part, int nsplit, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s);
 // column sums: out[c] = sum over rows of part[row][c]; and of a stored tensor, in two steps

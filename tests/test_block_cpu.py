@@ -34,11 +34,11 @@ def test_linear_refusals(L):
         assert _linear(L, **bad) == B.WINO_ERR_ALIGN, bad
     for bad in (dict(y=X), dict(y=W), dict(y=X + 16), dict(y=BIAS), dict(r=Y + 16), dict(r=Y, ldr=16), dict(r=Y, ldy=16)):
         assert _linear(L, **bad) == B.WINO_ERR_ALIAS, bad
-    need = B.wino_linear_workspace_bytes(64, 64, 4096, B.WINO_F16)
+    need = B.wino_linear_workspace_bytes(80, 64, 4096, B.WINO_F16)
     assert need > 0
-    assert _linear(L, M=64, N=64, K=4096, n=need - 1) == B.WINO_ERR_WORKSPACE
-    assert _linear(L, M=64, N=64, K=4096, ws=None) == B.WINO_ERR_WORKSPACE
-    assert _linear(L, M=64, N=64, K=4096, ws=WS + 8) == B.WINO_ERR_ALIGN
+    assert _linear(L, M=80, N=64, K=4096, n=need - 1) == B.WINO_ERR_WORKSPACE
+    assert _linear(L, M=80, N=64, K=4096, ws=None) == B.WINO_ERR_WORKSPACE
+    assert _linear(L, M=80, N=64, K=4096, ws=WS + 8) == B.WINO_ERR_ALIGN
 
 
 def _backward(L, which, x=X, w=W, b=BIAS, dy=Y, dx=DX, dw=DW, db=DB, M=4, N=8, K=16, ldx=None, lddy=None, lddx=None, dt=B.WINO_F16, act=2, ws=WS, n=BIG):
@@ -122,6 +122,19 @@ def test_attention_refusals(L, backward):
         need = B.wino_attention_workspace_bytes(1, 1, 9000, 1, 1, 64, B.WINO_F16)
         assert need > 0 and call(n=need - 1, **long) == B.WINO_ERR_WORKSPACE and call(ws=None, **long) == B.WINO_ERR_WORKSPACE
     assert call(lse=0xa0000002) == B.WINO_ERR_ALIGN and call(kv_len=0xa1000002) == B.WINO_ERR_ALIGN
+
+
+def test_packed_arguments_are_the_struct():
+    assert B._ATTENTION_ARGS.size == ctypes.sizeof(B.wino_attention_args)
+    import torch
+    q, k = torch.zeros(2, 3, 4, 16), torch.zeros(2, 5, 2, 16)
+    lse, lens, mask = torch.zeros(2, 4, 3), torch.zeros(2, dtype=torch.int32), torch.zeros(2, 5, dtype=torch.uint8)
+    a = B.wino_attention_args.from_buffer_copy(B._attention(q, k, k, q, lse, lens, mask, 0.5, (q, q, k, k)))
+    assert (a.B, a.Sq, a.Skv, a.H, a.Hkv, a.D, a.dtype, a.scale) == (2, 3, 5, 4, 2, 16, B.WINO_F32, 0.5)
+    assert (a.lse, a.kv_len, a.key_mask) == (lse.data_ptr(), lens.data_ptr(), mask.data_ptr())
+    for name in NAMES:
+        t, want = getattr(a, name), k if name in ("k", "v", "dk", "dv") else q
+        assert (t.data, t.stride_b, t.stride_s, t.stride_h) == (want.data_ptr(), *want.stride()[:3]), name
 
 
 def test_sizes_of_bad_arguments_are_zero(L):
