@@ -45,23 +45,25 @@ BackwardSpace backward_space(int M, int W, int K, int dt, bool stored) {
     b.dz = stored ? up256((size_t)M * b.ld * bytes_of(dt)) : 0;
     b.sum_rows = stored ? gemm_most_sum_rows(M) : column_sum_rows(M);
     b.sums = up256((size_t)b.sum_rows * W * sizeof(float));
-    const size_t px = product_bytes(M, K, W, dt), pw = product_bytes(W, K, M, dt);
-    b.parts = px > pw ? px : pw;
+    b.parts = product_bytes(M, K, W, dt) + product_bytes(W, K, M, dt);
     b.total = b.dz + b.sums + b.parts;
     return b;
 }
 
-// dx = dz w and dw = dz^T x
+// dx = dz w and dw = dz^T x, in one launch where both are asked for
 int run_products(const void* x, long long ldx, const void* w, const void* dz, long long lddz, void* dx, long long lddx, void* dw, int M, int W, int K, void* scratch, int dt, hipStream_t s) {
-    Epilogue e;
-    if (dx) {
-        e.out = dx; e.ld_out = lddx;
-        if (product(EP_STORE, true, false, Operand{w, K}, Operand{dz, lddz}, GemmShape{M, K, W}, e, scratch, dt, s) != hipSuccess) return WINO_ERR_HIP;
-    }
-    if (dw) {
-        e.out = dw; e.ld_out = K;
-        if (product(EP_STORE, true, true, Operand{x, ldx}, Operand{dz, lddz}, GemmShape{W, K, M}, e, scratch, dt, s) != hipSuccess) return WINO_ERR_HIP;
-    }
+    Product a{Operand{w, K}, Operand{dz, lddz}, GemmShape{M, K, W}, Epilogue(), gemm_ranges(M, K, W, dt)};
+    Product b{Operand{x, ldx}, Operand{dz, lddz}, GemmShape{W, K, M}, Epilogue(), gemm_ranges(W, K, M, dt)};
+    a.e.out = dx; a.e.ld_out = lddx;
+    b.e.out = dw; b.e.ld_out = K;
+    if (!dw) return product(EP_STORE, true, false, a.P, a.Q, a.g, a.e, scratch, dt, s) == hipSuccess ? WINO_OK : WINO_ERR_HIP;
+    if (!dx) return product(EP_STORE, true, true, b.P, b.Q, b.g, b.e, scratch, dt, s) == hipSuccess ? WINO_OK : WINO_ERR_HIP;
+    unsigned char* base = static_cast<unsigned char*>(scratch);
+    if (a.nsplit > 1) a.e.part = reinterpret_cast<float*>(base);
+    if (b.nsplit > 1) b.e.part = reinterpret_cast<float*>(base + product_bytes(M, K, W, dt));
+    if (launch_gemm_pair(a, b, dt, s) != hipSuccess) return WINO_ERR_HIP;
+    for (const Product* p : {&a, &b})
+        if (p->nsplit > 1 && launch_join(p->e.part, p->nsplit, p->g, p->e, dt, s) != hipSuccess) return WINO_ERR_HIP;
     return WINO_OK;
 }
 
@@ -101,10 +103,11 @@ int products_backward(const void* x, const void* w, const float* bias, const voi
         e.bias = bias; e.extra = dy; e.ld_extra = lddy; e.out = base; e.ld_out = b.ld; e.sums = sums; e.act = act;
         if (launch_gemm(halves == 2 ? EP_DGLU : EP_DLINEAR, false, false, Operand{w, K}, Operand{x, ldx}, GemmShape{M, N, K}, e, 1, dt, s, &b.sum_rows) != hipSuccess) return WINO_ERR_HIP;
         dz = base; lddz = b.ld;
-    } else if (dbias && launch_column_sums(dy, lddy, M, N, sums, dt, s) != hipSuccess) {
+    } else if (dbias && launch_column_sums(dy, lddy, M, N, b.sum_rows == 1 ? dbias : sums, dt, s) != hipSuccess) {
         return WINO_ERR_HIP;
     }
-    if (dbias && launch_sum_rows(sums, b.sum_rows, W, dbias, s) != hipSuccess) return WINO_ERR_HIP;
+    if (dbias && (stored || b.sum_rows > 1) && launch_sum_rows(sums, b.sum_rows, W, dbias, s) != hipSuccess) return WINO_ERR_HIP;
+    if (!dx && !dw) return WINO_OK;
     return run_products(x, ldx, w, dz, lddz, dx, lddx, dw, M, W, K, base + b.dz + b.sums, dt, s);
 }
 

@@ -39,6 +39,9 @@ struct Epilogue {
 // M rows and N columns of out (EP_GLU / EP_DGLU: N gate pairs, P has 2N rows), reduction length K.
 struct GemmShape { int M, N, K; };
 
+// A product with its ranges: e.part set where there are several.
+struct Product { Operand P, Q; GemmShape g; Epilogue e; int nsplit; };
+
 bool gemm_dims_ok(long long M, long long N, long long K);
 // rows of Epilogue::sums that a launch with EP_DLINEAR / EP_DGLU may fill; launch_gemm says how many it did (sum_rows, may be null)
 int gemm_most_sum_rows(int M);
@@ -46,6 +49,8 @@ int gemm_most_sum_rows(int M);
 int gemm_ranges(int M, int N, int K, int dt);
 hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit,
                        int dt, hipStream_t s, int* sum_rows = nullptr);
+// a = dz w (P across, Q along the reduction) and b = dz^T x (both across), with EP_STORE or ranges
+hipError_t launch_gemm_pair(const Product& a, const Product& b, int dt, hipStream_t s);
 // x W^T with EP_LINEAR or (glu) EP_GLU for few rows, one kernel, no workspace
 bool few_gemm_ok(int M);
 hipError_t launch_few_gemm(bool glu, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s);
@@ -53,7 +58,7 @@ hipError_t launch_few_gemm(bool glu, const Operand& P, const Operand& Q, const G
 hipError_t launch_join(const float* part, int nsplit, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s);
 // column sums: out[c] = sum over rows of part[row][c]; and of a stored tensor, in two steps
 hipError_t launch_sum_rows(const float* part, int rows, int cols, float* out, hipStream_t s);
-int column_sum_rows(int M);
+int column_sum_rows(int M);          // 1: launch_column_sums writes the sums themselves
 hipError_t launch_column_sums(const void* x, long long ld, int M, int N, float* part, int dt, hipStream_t s);
 
 // One call of the attention operators; strides in elements, the last dimension contiguous.

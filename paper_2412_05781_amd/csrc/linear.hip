@@ -255,10 +255,19 @@ template <typename E, int ACT> __global__ void __launch_bounds__(256) join_kerne
     const int n0 = (int)(id - m * quads) * 4;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     const size_t step = (size_t)g.M * g.N;
-    for (int r = 0; r < nsplit; ++r)
+    const float* p = part + (size_t)m * g.N + n0;
+    if (g.N % 4 == 0) {
+#pragma unroll 4
+        for (int r = 0; r < nsplit; ++r) {
+            const float4 v = *reinterpret_cast<const float4*>(p + (size_t)r * step);
+            s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+        }
+    } else {
+        for (int r = 0; r < nsplit; ++r)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n0 + i < g.N) s[i] += part[(size_t)r * step + (size_t)m * g.N + n0 + i];
+            for (int i = 0; i < 4; ++i)
+                if (n0 + i < g.N) s[i] += p[(size_t)r * step + i];
+    }
     const bool whole = rows_whole<E>(g, e);
     if (linear) finish4<E, EP_LINEAR, ACT>(g, e, m, n0, s, s, whole, nullptr, nullptr);
     else finish4<E, EP_STORE, ACT>(g, e, m, n0, s, s, whole, nullptr, nullptr);
@@ -282,17 +291,40 @@ __global__ void __launch_bounds__(1024) sum_rows_kernel(const float* part, int r
     }
 }
 
-// 64 columns x a range of rows per workgroup
-template <typename E> __global__ void __launch_bounds__(256) column_sums_kernel(const E* x, long long ld, int M, int N, float* part) {
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
+// 64 columns x a range of rows per workgroup; eight lanes a row, eight rows a wave at a time
+template <typename E> __global__ void __launch_bounds__(256) column_sums_kernel(const E* x, long long ld, int M, int N, float* part, bool vec) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c0 = blockIdx.x * 64 + (lane & 7) * 8, left = N - c0;
     const long long r0 = (long long)blockIdx.y * M / gridDim.y, r1 = (long long)(blockIdx.y + 1) * M / gridDim.y;
     __shared__ float t[4][64];
-    float a = 0.f;
-    if (c < N)
-        for (long long r = r0 + w; r < r1; r += 4) a += to_f32<E>(x[r * ld + c]);
-    t[w][threadIdx.x & 63] = a;
+    float a[8] = {};
+    if (vec && left >= 8) {
+#pragma unroll 4
+        for (long long r = r0 + w * 8 + (lane >> 3); r < r1; r += 32) {
+            const E* p = x + r * ld + c0;
+            if constexpr (sizeof(E) == 4) {
+                const float4 u = reinterpret_cast<const float4*>(p)[0], v = reinterpret_cast<const float4*>(p)[1];
+                a[0] += u.x; a[1] += u.y; a[2] += u.z; a[3] += u.w; a[4] += v.x; a[5] += v.y; a[6] += v.z; a[7] += v.w;
+            } else {
+                const uint4 u = *reinterpret_cast<const uint4*>(p);
+                a[0] += lo16<E>(u.x); a[1] += hi16<E>(u.x); a[2] += lo16<E>(u.y); a[3] += hi16<E>(u.y);
+                a[4] += lo16<E>(u.z); a[5] += hi16<E>(u.z); a[6] += lo16<E>(u.w); a[7] += hi16<E>(u.w);
+            }
+        }
+    } else {
+        for (long long r = r0 + w * 8 + (lane >> 3); r < r1; r += 32)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) a[i] += to_f32<E>(x[r * ld + c0 + i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int d = 8; d < 64; d <<= 1) a[i] += __shfl_xor(a[i], d);
+        if (lane < 8) t[w][lane * 8 + i] = a[i];
+    }
     __syncthreads();
-    if (w == 0 && c < N) part[(size_t)blockIdx.y * N + c] = (t[0][threadIdx.x] + t[1][threadIdx.x]) + (t[2][threadIdx.x] + t[3][threadIdx.x]);
+    const int c = blockIdx.x * 64 + threadIdx.x;
+    if (threadIdx.x < 64 && c < N) part[(size_t)blockIdx.y * N + c] = (t[0][threadIdx.x] + t[1][threadIdx.x]) + (t[2][threadIdx.x] + t[3][threadIdx.x]);
 }
 
 }  // namespace
@@ -303,19 +335,29 @@ bool gemm_dims_ok(long long M, long long N, long long K) {
            ((M + kBQ - 1) / kBQ) * ((N + kBP / 2 - 1) / (kBP / 2)) <= (1LL << 26);
 }
 
-// workgroups of 64 rows with two waves across them, of 128 with two or of 256 with four
+// one row of sums per 32 rows, per 64 rows twice, per 128 rows twice or four times, or per 256 rows four times
 int gemm_most_sum_rows(int M) { return (M + 63) / 64 * 2 + 4; }
 
-// A reduction is cut where there are fewer tiles than compute units, into ranges long enough to be worth the join (two-byte types: sixteen stages,
-// about 5 us; fp32, whose stages last four times as long: four).
+// How many ranges a reduction is cut into.  Two-byte types: where there are fewer 64x64 tiles than the chip holds, down to ranges of sixteen stages (about
+// 5 us), which are worth the join.  fp32 is bound by its MFMAs, 0.49 us a stage of a 64x64 tile and compute unit, and what counts is how evenly the tiles
+// fill the units: the number with the least time in rounds of workgroups, the join's traffic counted (2028 x 2560 x 640, 320 tiles: one range
+// 88 us, two 76, four 72 with a join of single loads).
 int gemm_ranges(int M, int N, int K, int dt) {
     auto tiles = [&](int n, int m) { return (((long long)N + n - 1) / n) * (((long long)M + m - 1) / m); };
-    const bool f32 = dt == DT_F32;
-    const int stages = K / (f32 ? 32 : 64);
-    if (!f32 && tiles(128, 128) >= 130) return 1;
-    long long n = f32 ? 512 / tiles(kBP, kBQ) : 768 / tiles(64, 64);
-    const int most = stages / (f32 ? 4 : 16);
-    if (n > most) n = most;
+    const long long t64 = tiles(64, 64);
+    if (dt == DT_F32) {
+        const int stages = (K + 31) / 32;
+        int best = 1;
+        double least = 0.;
+        for (int n = 1; n <= 8 && (n == 1 || stages / n >= 8); ++n) {
+            const double us = 0.49 * (double)((t64 * n + 255) / 256) * ((stages + n - 1) / n) + (n == 1 ? 0. : 4. + (double)n * M * N * 8. / 4e6);
+            if (n == 1 || us < least) { best = n; least = us; }
+        }
+        return best;
+    }
+    if (tiles(128, 128) >= 130) return 1;
+    long long n = 768 / t64;
+    if (n > K / 64 / 16) n = K / 64 / 16;
     if (n > 16) n = 16;
     return n < 2 ? 1 : (int)n;
 }
@@ -336,6 +378,13 @@ hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, con
             default: return hipErrorInvalidValue;
         }
     });
+}
+
+hipError_t launch_gemm_pair(const Product& a, const Product& b, int dt, hipStream_t s) {
+    const int ea = a.e.part ? EP_PART : EP_STORE, eb = b.e.part ? EP_PART : EP_STORE;
+    if (tile_gemm_ok(ea, true, false, a.P, a.Q, a.g, a.e, dt) && tile_gemm_ok(eb, true, true, b.P, b.Q, b.g, b.e, dt)) return launch_tile_pair(a, b, dt, s);
+    const hipError_t rc = launch_gemm(ea, true, false, a.P, a.Q, a.g, a.e, a.nsplit, dt, s);
+    return rc != hipSuccess ? rc : launch_gemm(eb, true, true, b.P, b.Q, b.g, b.e, b.nsplit, dt, s);
 }
 
 hipError_t launch_join(const float* part, int nsplit, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s) {
@@ -360,12 +409,13 @@ hipError_t launch_sum_rows(const float* part, int rows, int cols, float* out, hi
     return hipGetLastError();
 }
 
-int column_sum_rows(int M) { return M < 64 ? 1 : M < 64 * 128 ? M / 64 : 128; }
+int column_sum_rows(int M) { return M <= 1024 ? 1 : M < 256 * 64 ? M / 256 : 64; }
 
 hipError_t launch_column_sums(const void* x, long long ld, int M, int N, float* part, int dt, hipStream_t s) {
     return with_dtype(dt, [&](auto* tag) -> hipError_t {
         using E = std::remove_pointer_t<decltype(tag)>;
-        hipLaunchKernelGGL((column_sums_kernel<E>), dim3((unsigned)((N + 63) / 64), (unsigned)column_sum_rows(M)), dim3(256), 0, s, (const E*)x, ld, M, N, part);
+        hipLaunchKernelGGL((column_sums_kernel<E>), dim3((unsigned)((N + 63) / 64), (unsigned)column_sum_rows(M)), dim3(256), 0, s, (const E*)x, ld, M, N, part,
+                           ((reinterpret_cast<uintptr_t>(x) | (uintptr_t)(ld * (long long)sizeof(E))) & 15u) == 0);
         return hipGetLastError();
     });
 }

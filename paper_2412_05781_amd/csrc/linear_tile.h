@@ -92,9 +92,11 @@ template <typename E> inline bool vec_rows(const Operand& o) {
     return ((reinterpret_cast<uintptr_t>(o.p) | (uintptr_t)(o.ld * (long long)sizeof(E))) & 15u) == 0;
 }
 
-// The kernel for two-byte types with operands that can be fetched 16 bytes at a time (linear_tile.hip): whether it takes a call, the rows of column sums it
-// fills, the ranges it cuts the reduction into, and the launch.
+// The kernel for operands that can be fetched 16 bytes at a time (linear_tile.hip): whether it takes a call, and the launch.
 bool tile_gemm_ok(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int dt);
 hipError_t launch_tile_gemm(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, int dt, hipStream_t s, int* sum_rows);
+
+// two products in one launch: a with P across and Q along the reduction, b with both across
+hipError_t launch_tile_pair(const Product& a, const Product& b, int dt, hipStream_t s);
 
 }  // namespace wino

@@ -1,7 +1,7 @@
-// The matrix kernel of the transformer-block operators for two-byte types whose operands can be fetched 16 bytes at a time: global -> LDS transfers
-// without a detour through registers, a ring of stages of 64 reduction elements, eight or four waves that own 32x32 MFMA tiles.
+// The matrix kernel of the transformer-block operators for operands that can be fetched 16 bytes at a time: global -> LDS transfers without a
+// detour through registers, a ring of stages of 128 bytes of reduction elements (64, fp32: 32), four to eight waves that own 32x32 MFMA tiles.
 //
-// A stage of an operand that runs along the reduction is BI rows of 128 bytes, of one across it 64 rows of BI elements; both are filled by transfers of
+// A stage of an operand that runs along the reduction is BI rows of 128 bytes, of one across it 64 (fp32: 32) rows of BI elements; both are filled by transfers of
 // 1 KB whose lanes fetch from swizzled places, so that the fragment reads (ds_read_b128, or the transposing ds_read_b64_tr_b16) find every bank
 // once.  Rows behind the edge are fetched from the last row inside (their sums are not stored), reduction elements behind the end from 16 zero bytes.
 #include "linear_tile.h"
@@ -28,12 +28,30 @@ __device__ __forceinline__ float sum_over_16(float v) {
 }
 
 // eight neighbouring elements of a row
-template <typename E> __device__ __forceinline__ void unpack8(const uint4& f, float* v) {
-    v[0] = lo16<E>(f.x); v[1] = hi16<E>(f.x); v[2] = lo16<E>(f.y); v[3] = hi16<E>(f.y);
-    v[4] = lo16<E>(f.z); v[5] = hi16<E>(f.z); v[6] = lo16<E>(f.w); v[7] = hi16<E>(f.w);
+template <typename E> struct Eight { uint4 w[sizeof(E) / 2]; };
+template <typename E> __device__ __forceinline__ Eight<E> load8(const E* p) {
+    Eight<E> f;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(E) / 2; ++i) f.w[i] = reinterpret_cast<const uint4*>(p)[i];
+    return f;
+}
+template <typename E> __device__ __forceinline__ void unpack8(const Eight<E>& e, float* v) {
+    if constexpr (sizeof(E) == 4) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) { v[4 * i] = __uint_as_float(e.w[i].x); v[4 * i + 1] = __uint_as_float(e.w[i].y); v[4 * i + 2] = __uint_as_float(e.w[i].z); v[4 * i + 3] = __uint_as_float(e.w[i].w); }
+    } else {
+        const uint4& f = e.w[0];
+        v[0] = lo16<E>(f.x); v[1] = hi16<E>(f.x); v[2] = lo16<E>(f.y); v[3] = hi16<E>(f.y);
+        v[4] = lo16<E>(f.z); v[5] = hi16<E>(f.z); v[6] = lo16<E>(f.w); v[7] = hi16<E>(f.w);
+    }
 }
 template <typename E> __device__ __forceinline__ void store8(E* p, const float* v) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack2<E>(v[0], v[1]), pack2<E>(v[2], v[3]), pack2<E>(v[4], v[5]), pack2<E>(v[6], v[7]));
+    if constexpr (sizeof(E) == 4) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+        *reinterpret_cast<uint4*>(p) = make_uint4(pack2<E>(v[0], v[1]), pack2<E>(v[2], v[3]), pack2<E>(v[4], v[5]), pack2<E>(v[6], v[7]));
+    }
 }
 
 // Epilogue of one wave's tile.  acc[i][j]: rows n of 32-row block i (GLU: block i of the up rows, FP / 2 + i of the gate rows), columns m of block j.
@@ -45,7 +63,7 @@ __device__ __forceinline__ void finish_tile(const GemmShape& g, const Epilogue& 
     const int half = lane >> 5;
     E* out = static_cast<E*>(e.out);
     const E* extra = static_cast<const E*>(e.extra);
-    const bool has_bias = EP != EP_STORE && EP != EP_PART && e.bias, has_extra = SUMS || (EP == EP_LINEAR && extra);
+    const bool has_bias = EP != EP_STORE && e.bias, has_extra = SUMS || (EP == EP_LINEAR && extra);
     long long mrow[FQ];
     bool m_on[FQ];
 #pragma unroll
@@ -59,7 +77,7 @@ __device__ __forceinline__ void finish_tile(const GemmShape& g, const Epilogue& 
         int n[2];
         bool n_on[2];
         float bias[2][8] = {}, bias2[2][8] = {};
-        uint4 ex[2][FQ] = {};
+        Eight<E> ex[2][FQ] = {};
 #pragma unroll
         for (int qp = 0; qp < 2; ++qp) {
             // after the exchange of halves a lane holds n .. n + 7 of its row; N is a multiple of 8 here
@@ -75,7 +93,7 @@ __device__ __forceinline__ void finish_tile(const GemmShape& g, const Epilogue& 
             }
             if (has_extra) {
 #pragma unroll
-                for (int j = 0; j < FQ; ++j) ex[qp][j] = *reinterpret_cast<const uint4*>(extra + mrow[j] * e.ld_extra + n[qp]);
+                for (int j = 0; j < FQ; ++j) ex[qp][j] = load8<E>(extra + mrow[j] * e.ld_extra + n[qp]);
             }
         }
 #pragma unroll
@@ -96,7 +114,7 @@ __device__ __forceinline__ void finish_tile(const GemmShape& g, const Epilogue& 
                     }
                 }
                 const bool on = n_on[qp] && m_on[j];
-                if constexpr (EP == EP_PART) {
+                if (EP == EP_STORE && e.part) {            // uniform: one of several ranges
                     float* p = e.part + ((long long)split * g.M + mrow[j]) * g.N + n[qp];
                     if (on) {
                         *reinterpret_cast<float4*>(p) = make_float4(s[0], s[1], s[2], s[3]);
@@ -182,6 +200,38 @@ template <typename E, int BI, int F, int W> struct Fragments<E, false, BI, F, W>
     }
     __device__ __forceinline__ u32x4_t get(int i) const { return f[i]; }
 };
+template <int OFF> __device__ __forceinline__ void lds_read4_async(uint32_t& dst, uint32_t addr) {
+    asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(OFF));
+}
+template <int BI, int F, int W> struct Fragments<float, true, BI, F, W> {
+    static constexpr int READS = 4 * F;
+    struct Place { uint32_t base[F]; };
+    uint32_t f[F][4];
+    static __device__ __forceinline__ Place place(uint32_t tile, int w, int lane) {
+        Place p;
+        const int row = 4 * (lane >> 5);                                                         // three rows further, or eight: the same swizzle
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            const int col = (i * W + w) * 32 + (lane & 31);
+            p.base[i] = tile + (uint32_t)(row * (BI * 4) + (((col >> 2) ^ swz_across<float, BI>(row)) << 4) + ((col & 3) << 2));
+        }
+        return p;
+    }
+    template <int KS> __device__ __forceinline__ void read(const Place& p, uint32_t slot) {
+        static_for<F>([&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            const uint32_t at = p.base[i] + slot;
+            static_for<4>([&](auto jc) { constexpr int j = decltype(jc)::value; lds_read4_async<(KS * 8 + j) * BI * 4>(f[i][j], at); });
+        });
+    }
+    __device__ __forceinline__ void pin_all() {
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(f[i][j]));
+    }
+    __device__ __forceinline__ u32x4_t get(int i) const { return u32x4_t{f[i][0], f[i][1], f[i][2], f[i][3]}; }
+};
 template <typename E, int BI, int F, int W> struct Fragments<E, true, BI, F, W> {
     static constexpr int READS = 2 * F;
     struct Place { uint32_t base[F]; };
@@ -213,8 +263,9 @@ template <typename E, int BI, int F, int W> struct Fragments<E, true, BI, F, W> 
 
 // BP rows of P x BQ rows of Q per workgroup of WP x WQ waves, ring of NST stages.
 template <typename E, int EP, bool PA, bool QA, int BP, int BQ, int WP, int WQ, int NST>
-__global__ void __launch_bounds__(WP * WQ * 64) gemm_tile_kernel(Operand P, Operand Q, GemmShape g, Epilogue e, int tiles_p, int tiles_q, int total, int per_xcd, int nsplit) {
+__device__ __forceinline__ void gemm_tile(const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int tiles_p, int tiles_q, int nsplit, int logical, unsigned char* lds) {
     constexpr bool GLU = EP == EP_GLU || EP == EP_DGLU;
+    constexpr int ES = (int)sizeof(E), V = 16 / ES, KEL = 128 / ES;              // elements per chunk, reduction elements per stage
     constexpr int NW = WP * WQ, FP = BP / (32 * WP), FQ = BQ / (32 * WQ);
     constexpr int P_BYTES = BP * 128, STAGE = (BP + BQ) * 128;
     constexpr int LP = BP / 8 / NW, LQ = BQ / 8 / NW;      // 1 KB transfers per wave and stage
@@ -222,10 +273,6 @@ __global__ void __launch_bounds__(WP * WQ * 64) gemm_tile_kernel(Operand P, Oper
     // MFMA steps whose fragments are requested together: a group's MFMAs have to last as long as the next group's reads
     constexpr int KH = FP * FQ >= 8 ? 1 : 2, NG = 4 / KH;
     static_assert(BP % (8 * NW) == 0 && BQ % (8 * NW) == 0, "whole transfers");
-    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-
-    const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
-    if (logical >= total) return;                          // uniform per workgroup, before any barrier
     const int split = logical / (tiles_p * tiles_q), in = logical - split * (tiles_p * tiles_q);
     // Eight tiles of Q against each tile of P in turn: the 32 to 64 workgroups that an XCD runs at a time then share tiles of both operands in its L2.
     constexpr int GROUP = 8;
@@ -234,13 +281,13 @@ __global__ void __launch_bounds__(WP * WQ * 64) gemm_tile_kernel(Operand P, Oper
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
     const int n0 = bp * BN;
     const long long m0 = (long long)bq * BQ;
-    const int nk = (g.K + 63) / 64;
+    const int nk = (g.K + KEL - 1) / KEL;
     const int kt0 = (int)((long long)split * nk / nsplit), kt1 = (int)((long long)(split + 1) * nk / nsplit), stages = kt1 - kt0;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte_t*)lds;
 
     // Where transfer i of this wave fetches: a wave-uniform base that moves with the stage and a byte offset per lane.
-    const unsigned char* sp = static_cast<const unsigned char*>(P.p) + (PA ? ((long long)kt0 * 64 * P.ld + n0) * 2 : ((long long)n0 * P.ld + (long long)kt0 * 64) * 2);
-    const unsigned char* sq = static_cast<const unsigned char*>(Q.p) + (QA ? ((long long)kt0 * 64 * Q.ld + m0) * 2 : (m0 * Q.ld + (long long)kt0 * 64) * 2);
+    const unsigned char* sp = static_cast<const unsigned char*>(P.p) + (PA ? (long long)kt0 * KEL * P.ld + n0 : (long long)n0 * P.ld + (long long)kt0 * KEL) * ES;
+    const unsigned char* sq = static_cast<const unsigned char*>(Q.p) + (QA ? (long long)kt0 * KEL * Q.ld + m0 : m0 * Q.ld + (long long)kt0 * KEL) * ES;
     uint32_t op[LP], oq[LQ];
     int kp[LP], kq[LQ];                                    // first reduction element of the lane's chunk within a stage
 #pragma unroll
@@ -251,13 +298,13 @@ __global__ void __launch_bounds__(WP * WQ * 64) gemm_tile_kernel(Operand P, Oper
             int r = row;                                   // row of P, relative to n0
             if (GLU && row >= BP / 2) { r = row - BP / 2; r = (n0 + r < g.N ? r : g.N - 1 - n0) + g.N; }
             else r = n0 + r < g.N ? r : g.N - 1 - n0;
-            op[i] = (uint32_t)r * (uint32_t)(P.ld * 2) + (uint32_t)chunk * 16u;
-            kp[i] = chunk * 8;
+            op[i] = (uint32_t)r * (uint32_t)(P.ld * ES) + (uint32_t)chunk * 16u;
+            kp[i] = chunk * V;
         } else {
-            constexpr int CPR = BP / 8, RPT = 64 / CPR;
+            constexpr int CPR = BP / V, RPT = 64 / CPR;
             const int row = t * RPT + lane / CPR, chunk = (lane % CPR) ^ swz_across<E, BP>(row);
-            const int c = n0 + chunk * 8 < g.N ? chunk * 8 : g.N - 8 - n0;
-            op[i] = (uint32_t)row * (uint32_t)(P.ld * 2) + (uint32_t)(c * 2);
+            const int c = n0 + chunk * V < g.N ? chunk * V : g.N - V - n0;
+            op[i] = (uint32_t)row * (uint32_t)(P.ld * ES) + (uint32_t)(c * ES);
             kp[i] = row;
         }
     }
@@ -267,27 +314,27 @@ __global__ void __launch_bounds__(WP * WQ * 64) gemm_tile_kernel(Operand P, Oper
         if constexpr (!QA) {
             const int row = t * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
             const int r = m0 + row < g.M ? row : (int)(g.M - 1 - m0);
-            oq[i] = (uint32_t)r * (uint32_t)(Q.ld * 2) + (uint32_t)chunk * 16u;
-            kq[i] = chunk * 8;
+            oq[i] = (uint32_t)r * (uint32_t)(Q.ld * ES) + (uint32_t)chunk * 16u;
+            kq[i] = chunk * V;
         } else {
-            constexpr int CPR = BQ / 8, RPT = 64 / CPR;
+            constexpr int CPR = BQ / V, RPT = 64 / CPR;
             const int row = t * RPT + lane / CPR, chunk = (lane % CPR) ^ swz_across<E, BQ>(row);
-            const int c = m0 + chunk * 8 < g.M ? chunk * 8 : (int)(g.M - 8 - m0);
-            oq[i] = (uint32_t)row * (uint32_t)(Q.ld * 2) + (uint32_t)(c * 2);
+            const int c = m0 + chunk * V < g.M ? chunk * V : (int)(g.M - V - m0);
+            oq[i] = (uint32_t)row * (uint32_t)(Q.ld * ES) + (uint32_t)(c * ES);
             kq[i] = row;
         }
     }
-    const long long step_p = PA ? 64 * P.ld * 2 : 128, step_q = QA ? 64 * Q.ld * 2 : 128;
+    const long long step_p = PA ? KEL * P.ld * ES : 128, step_q = QA ? KEL * Q.ld * ES : 128;
     int next = kt0;                                        // next stage to fetch
     auto issue = [&](int slot) {
         const uint32_t dst = lds0 + (uint32_t)slot * STAGE + (uint32_t)wave * 1024u;
-        const int left = g.K - next * 64;                  // reduction elements from this stage on
-        if (left >= 64) {
+        const int left = g.K - next * KEL;                  // reduction elements from this stage on
+        if (left >= KEL) {
 #pragma unroll
             for (int i = 0; i < LP; ++i) dma_load_1k_s(sp, op[i], dst + (uint32_t)(NW * i) * 1024u);
 #pragma unroll
             for (int i = 0; i < LQ; ++i) dma_load_1k_s(sq, oq[i], dst + P_BYTES + (uint32_t)(NW * i) * 1024u);
-        } else {                                           // K is a multiple of 8 where a chunk runs along it
+        } else {                                           // K is a multiple of a chunk where one runs along it
 #pragma unroll
             for (int i = 0; i < LP; ++i) dma_load_1k_v(kp[i] < left ? sp + op[i] : zero16, dst + (uint32_t)(NW * i) * 1024u);
 #pragma unroll
@@ -367,7 +414,7 @@ __global__ void __launch_bounds__(WP * WQ * 64) gemm_tile_kernel(Operand P, Oper
     }
 
     const long long sum_row = (long long)bq * WQ + wq;
-    if constexpr (EP == EP_STORE || EP == EP_PART) {
+    if constexpr (EP == EP_STORE) {
         finish_tile<E, EP, ACT_NONE, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split);
     } else {
         switch (e.act) {                                   // uniform
@@ -376,6 +423,30 @@ __global__ void __launch_bounds__(WP * WQ * 64) gemm_tile_kernel(Operand P, Oper
             case ACT_GELU: finish_tile<E, EP, ACT_GELU, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split); break;
             default: finish_tile<E, EP, ACT_GELU_TANH, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split); break;
         }
+    }
+}
+
+template <typename E, int EP, bool PA, bool QA, int BP, int BQ, int WP, int WQ, int NST>
+__global__ void __launch_bounds__(WP * WQ * 64) gemm_tile_kernel(Operand P, Operand Q, GemmShape g, Epilogue e, int tiles_p, int tiles_q, int total, int per_xcd, int nsplit) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+    if (logical >= total) return;                          // uniform per workgroup, before any barrier
+    gemm_tile<E, EP, PA, QA, BP, BQ, WP, WQ, NST>(P, Q, g, e, tiles_p, tiles_q, nsplit, logical, lds);
+}
+
+// Two products in one launch, dz w (P across, Q along) and dz^T x (both across): either alone has few tiles and long reductions, together they fill the
+// chip.  XCD by XCD the first one's tiles, then the second one's.
+struct PairPart { Operand P, Q; GemmShape g; Epilogue e; int tiles_p, tiles_q, total, per_xcd, nsplit; };
+template <typename E, int BP, int BQ, int WP, int WQ, int NST>
+__global__ void __launch_bounds__(WP * WQ * 64) gemm_pair_kernel(PairPart a, PairPart b) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int xcd = blockIdx.x % 8, at = blockIdx.x / 8;
+    if (at < a.per_xcd) {
+        const int logical = xcd * a.per_xcd + at;
+        if (logical < a.total) gemm_tile<E, EP_STORE, true, false, BP, BQ, WP, WQ, NST>(a.P, a.Q, a.g, a.e, a.tiles_p, a.tiles_q, a.nsplit, logical, lds);
+    } else {
+        const int logical = xcd * b.per_xcd + at - a.per_xcd;
+        if (logical < b.total) gemm_tile<E, EP_STORE, true, true, BP, BQ, WP, WQ, NST>(b.P, b.Q, b.g, b.e, b.tiles_p, b.tiles_q, b.nsplit, logical, lds);
     }
 }
 
@@ -403,15 +474,23 @@ template <typename E, int EP, bool PA, bool QA> hipError_t launch_shape(const Op
     constexpr bool GLU = EP == EP_GLU || EP == EP_DGLU;
     const long long width = GLU ? 2LL * g.N : g.N, t256 = ((width + 255) / 256) * ((g.M + 255) / 256) * nsplit, t128 = ((width + 127) / 128) * ((g.M + 127) / 128) * nsplit;
     const int depth = g.K / nsplit;
+    if constexpr (sizeof(E) == 4) {
+        // bound by its MFMAs: the large block only where its tiles fill the units evenly (4096^3 144 TFLOP/s of the library's 151)
+        if (t128 >= 768) return launch_cfg<E, EP, PA, QA, 128, 128, 2, 2, 2>(P, Q, g, e, nsplit, s, sum_rows);
+        if constexpr (GLU) return launch_cfg<E, EP, PA, QA, 128, 64, 2, 2, 2>(P, Q, g, e, nsplit, s, sum_rows);
+        else if (depth < 512) return launch_cfg<E, EP, PA, QA, 64, 64, 2, 2, 2>(P, Q, g, e, nsplit, s, sum_rows);
+        else return launch_cfg<E, EP, PA, QA, 64, 64, 2, 2, 3>(P, Q, g, e, nsplit, s, sum_rows);
+    } else {
     if (depth >= 1536 && t256 >= 224) return launch_cfg<E, EP, PA, QA, 256, 256, 2, 4, 2>(P, Q, g, e, nsplit, s, sum_rows);
     if (t128 >= 320) return launch_cfg<E, EP, PA, QA, 128, 128, 2, 4, 2>(P, Q, g, e, nsplit, s, sum_rows);
     if (t128 >= 130 && depth >= 1024) return launch_cfg<E, EP, PA, QA, 128, 128, 2, 4, 3>(P, Q, g, e, nsplit, s, sum_rows);
     if constexpr (GLU) return launch_cfg<E, EP, PA, QA, 128, 64, 2, 2, 3>(P, Q, g, e, nsplit, s, sum_rows);       // u and g in one wave: 64 rows of P each
     else return launch_cfg<E, EP, PA, QA, 64, 64, 2, 2, 3>(P, Q, g, e, nsplit, s, sum_rows);
+    }
 }
 
 template <typename E, int EP> hipError_t launch_layout(bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s, int* sum_rows) {
-    if constexpr (EP == EP_STORE || EP == EP_PART) {
+    if constexpr (EP == EP_STORE) {
         if (pa && qa) return launch_shape<E, EP, true, true>(P, Q, g, e, nsplit, s, sum_rows);
         if (pa) return launch_shape<E, EP, true, false>(P, Q, g, e, nsplit, s, sum_rows);
     }
@@ -420,8 +499,8 @@ template <typename E, int EP> hipError_t launch_layout(bool pa, bool qa, const O
 
 template <typename E> hipError_t launch_ep(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s, int* sum_rows) {
     switch (ep) {
-        case EP_STORE: return launch_layout<E, EP_STORE>(pa, qa, P, Q, g, e, nsplit, s, sum_rows);
-        case EP_PART: return launch_layout<E, EP_PART>(pa, qa, P, Q, g, e, nsplit, s, sum_rows);
+        case EP_STORE:
+        case EP_PART: return launch_layout<E, EP_STORE>(pa, qa, P, Q, g, e, nsplit, s, sum_rows);      // (told apart by e.part)
         case EP_LINEAR: return launch_layout<E, EP_LINEAR>(pa, qa, P, Q, g, e, nsplit, s, sum_rows);
         case EP_DLINEAR: return launch_layout<E, EP_DLINEAR>(pa, qa, P, Q, g, e, nsplit, s, sum_rows);
         case EP_GLU: return launch_layout<E, EP_GLU>(pa, qa, P, Q, g, e, nsplit, s, sum_rows);
@@ -430,23 +509,52 @@ template <typename E> hipError_t launch_ep(int ep, bool pa, bool qa, const Opera
     }
 }
 
+template <typename E, int BP, int BQ, int WP, int WQ, int NST> hipError_t launch_pair(PairPart a, PairPart b, hipStream_t s) {
+    constexpr int bytes = (BP + BQ) * 128 * NST;
+    static_assert(bytes <= 160 * 1024, "LDS budget");
+    for (PairPart* p : {&a, &b}) {
+        const long long tp = (p->g.N + BP - 1) / BP, tq = ((long long)p->g.M + BQ - 1) / BQ, total = tp * tq * p->nsplit;
+        if (total > 0x1fffffffLL) return hipErrorInvalidValue;
+        p->tiles_p = (int)tp; p->tiles_q = (int)tq; p->total = (int)total; p->per_xcd = (int)((total + 7) / 8);
+    }
+    auto kern = gemm_pair_kernel<E, BP, BQ, WP, WQ, NST>;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (attr != hipSuccess) return attr;
+    hipLaunchKernelGGL(kern, dim3((unsigned)((a.per_xcd + b.per_xcd) * 8)), dim3(WP * WQ * 64), bytes, s, a, b);
+    return hipGetLastError();
+}
+
+long long tiles128(const GemmShape& g) { return (((long long)g.N + 127) / 128) * (((long long)g.M + 127) / 128); }
+
 }  // namespace
 
+hipError_t launch_tile_pair(const Product& a, const Product& b, int dt, hipStream_t s) {
+    const PairPart pa{a.P, a.Q, a.g, a.e, 0, 0, 0, 0, a.nsplit}, pb{b.P, b.Q, b.g, b.e, 0, 0, 0, 0, b.nsplit};
+    const long long t128 = tiles128(a.g) * a.nsplit + tiles128(b.g) * b.nsplit;
+    return with_dtype(dt, [&](auto* tag) -> hipError_t {
+        using E = std::remove_pointer_t<decltype(tag)>;
+        if constexpr (sizeof(E) == 4) return t128 >= 768 ? launch_pair<E, 128, 128, 2, 2, 2>(pa, pb, s) : launch_pair<E, 64, 64, 2, 2, 3>(pa, pb, s);
+        else return t128 >= 256 ? launch_pair<E, 128, 128, 2, 4, 2>(pa, pb, s) : launch_pair<E, 64, 64, 2, 2, 3>(pa, pb, s);
+    });
+}
+
 bool tile_gemm_ok(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int dt) {
-    if (!two_byte(dt) || !vec_rows<__half>(P) || !vec_rows<__half>(Q)) return false;
+    const long long es = two_byte(dt) ? 2 : 4;
+    if (es == 2 ? !(vec_rows<__half>(P) && vec_rows<__half>(Q)) : !(vec_rows<float>(P) && vec_rows<float>(Q))) return false;
     const bool glu = ep == EP_GLU || ep == EP_DGLU;
-    if (g.N % 8 || (qa && g.M % 8) || (!(pa && qa) && g.K % 8)) return false;       // chunks of 16 bytes are whole; out's rows as well
+    const int v = es == 2 ? 8 : 4;
+    if (g.N % 8 || (qa && g.M % v) || (!(pa && qa) && g.K % v)) return false;       // chunks of 16 bytes are whole; out is written in eights
     // a lane's offset within a workgroup's rows is 32 bits wide
     const long long span_p = pa ? 64 : glu ? (long long)g.N + 256 : 256, span_q = qa ? 64 : 256;
-    if (P.ld * 2 * span_p >= (1LL << 31) || Q.ld * 2 * span_q >= (1LL << 31)) return false;
+    if (P.ld * es * span_p >= (1LL << 31) || Q.ld * es * span_q >= (1LL << 31)) return false;
     if (ep == EP_PART) return true;
-    uintptr_t bits = reinterpret_cast<uintptr_t>(e.out) | (uintptr_t)(e.ld_out * 2);
-    if (e.extra) bits |= reinterpret_cast<uintptr_t>(e.extra) | (uintptr_t)(e.ld_extra * 2);
+    uintptr_t bits = reinterpret_cast<uintptr_t>(e.out) | (uintptr_t)(e.ld_out * es);
+    if (e.extra) bits |= reinterpret_cast<uintptr_t>(e.extra) | (uintptr_t)(e.ld_extra * es);
     return (bits & 15) == 0;
 }
 
 hipError_t launch_tile_gemm(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, int dt, hipStream_t s, int* sum_rows) {
-    return dt == DT_F16 ? launch_ep<__half>(ep, pa, qa, P, Q, g, e, nsplit, s, sum_rows) : launch_ep<bf16_t>(ep, pa, qa, P, Q, g, e, nsplit, s, sum_rows);
+    return with_dtype(dt, [&](auto* tag) -> hipError_t { return launch_ep<std::remove_pointer_t<decltype(tag)>>(ep, pa, qa, P, Q, g, e, nsplit, s, sum_rows); });
 }
 
 }  // namespace wino
