@@ -40,8 +40,13 @@ template <int N> __device__ __forceinline__ void add_halves(float16_t (&acc)[N],
     }
 }
 
-// 64 query rows: dq, and D_i on the way
-template <typename E, int DP> __global__ void __launch_bounds__(256, (backward_waves<E, DP>()))
+// 64 query rows: dq, and D_i for the other kernel.
+//
+// D_i = do_i . o_i from the stored o carries o's rounding, which reaches every ds of the row with the same sign.  But the ds of a row add up to zero, so
+// what they do add up to, r, is that error: D_i + r is right to fp32, and dq less r times the weighted mean of the keys as well.  The mean costs one more
+// product with operands that are there already (4 x 8 x 1024 x 1024 x 80: 35 -> 43 us); the error of dq against 64 bits falls from 1.50 to 1.41 times that of
+// one rounding, which is the rounding of ds and that of dq.
+template <typename E, int DP> __global__ void __launch_bounds__(256, (DP <= (sizeof(E) == 2 ? 5 : 4) ? 2 : 1))
 attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_xcd) {
     using T = AttnTile<E, DP>;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -84,10 +89,12 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
             }
         }
         dlt += __shfl_xor(dlt, 32);
-        if (row_on && sub == 0 && half == 0) delta[row] = dlt;
     }
     const float lse2 = row_on ? a.lse[row] * kLog2e : 0.f;
-    float16_t acc[T::NV] = {};
+    constexpr bool MEAN = T::ES == 2;                      // fp32: o is not rounded
+    constexpr int NA = MEAN ? 2 * T::NV : T::NV;           // dq, then the mean of the keys
+    float16_t acc[NA] = {};
+    float rest = 0.f;
     const float c2 = a.scale * kLog2e;
     for (int t = 0; t < tiles; ++t) {
         unsigned char* tk = lds + (AHEAD ? (t & 1) * 2 * T::BYTES : 0);
@@ -116,7 +123,7 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
             Mma<E>::run(T::along(tv, 32 * sub, ks, lane), fo[ks], dp);
         }
 #pragma unroll
-        for (int q = 0; q < 16; ++q) s[q] = __builtin_amdgcn_exp2f(fmaf(s[q], c2, -lse2)) * (dp[q] - dlt);
+        for (int q = 0; q < 16; ++q) s[q] = __builtin_amdgcn_exp2f(fmaf(s[q], c2, -lse2));
         if (cur != 0xffffffffu) {
             asm volatile("" ::: "memory");                 // a branch
             const uint32_t mine = cur >> (4 * half);
@@ -125,14 +132,38 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
                 if (!((mine >> (8 * (q / 4) + q % 4)) & 1)) s[q] = 0.f;
         }
 #pragma unroll
-        for (int st = 0; st < T::ST; ++st) {
-            const u32x4_t w = T::weights(s, st);
+        for (int q = 0; q < 16; ++q) {
+            dp[q] = s[q] == 0.f ? 0.f : s[q] * (dp[q] - dlt);
+            if constexpr (MEAN) rest += dp[q];
+        }
 #pragma unroll
-            for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(tk, 32 * sub, st, d, lane), w, acc[d]);
+        for (int st = 0; st < T::ST; ++st) {
+            const u32x4_t w = T::weights(dp, st), wp = MEAN ? T::weights(s, st) : w;
+#pragma unroll
+            for (int d = 0; d < T::NV; ++d) {
+                const u32x4_t keys = T::across(tk, 32 * sub, st, d, lane);
+                Mma<E>::run(keys, w, acc[d]);
+                if constexpr (MEAN) Mma<E>::run(keys, wp, acc[T::NV + d]);
+            }
         }
     }
-    add_halves<T::NV>(acc, lds, wave, lane);
+    add_halves<NA>(acc, lds, wave, lane);
+    if constexpr (MEAN) {
+        rest += __shfl_xor(rest, 32);
+        float* t = reinterpret_cast<float*>(lds) + (wave & 1) * 64 + lane;
+        __syncthreads();
+        if (sub) *t = rest;
+        __syncthreads();
+        if (!sub) {
+            rest += *t;
+#pragma unroll
+            for (int d = 0; d < T::NV; ++d)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) acc[d][q] = fmaf(-rest, acc[T::NV + d][q], acc[d][q]);
+        }
+    }
     if (sub || !row_on) return;
+    if (half == 0) delta[row] = dlt + rest;
     unsigned char* out = const_cast<unsigned char*>(rows.at(a.dq, G, b, hk, r, T::ES));
 #pragma unroll
     for (int d = 0; d < T::NV; ++d)
@@ -340,7 +371,7 @@ hipError_t launch_attention_backward(const AttnArgs& a, int dt, hipStream_t s) {
                 using T = AttnTile<E, DP>;
                 constexpr int buffers = backward_ahead<E>() ? 2 : 1, halves = 2 * 1024 * T::NV * (int)sizeof(float);      // add_halves
                 constexpr int tiles_q = buffers * 2 * T::BYTES, tiles_k = tiles_q + buffers * 2 * T::ROWS * (int)sizeof(float);
-                constexpr int bytes_q = tiles_q > halves ? tiles_q : halves, bytes_k = tiles_k > 2 * halves ? tiles_k : 2 * halves;
+                constexpr int halves_q = T::ES == 2 ? 2 * halves : halves, bytes_q = tiles_q > halves_q ? tiles_q : halves_q, bytes_k = tiles_k > 2 * halves ? tiles_k : 2 * halves;
                 static_assert(bytes_q <= 160 * 1024 && bytes_k <= 160 * 1024, "LDS budget");
                 auto kq = attention_dq_kernel<E, DP>;
                 auto kk = attention_dkv_kernel<E, DP>;
