@@ -110,6 +110,12 @@ attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int tot
     const int r = tile * 128 + wave * 32 + (lane & 31);
     const bool row_on = r < rows.R;
 
+    u32x4_t fq[T::KS];                                     // first: under way while lengths and masks are looked at
+    {
+        const unsigned char* qrow = row_on ? rows.at(a.q, G, b, hk, r, T::ES) : nullptr;
+#pragma unroll
+        for (int ks = 0; ks < T::KS; ++ks) fq[ks] = load_channels<E>(qrow, (2 * ks + half) * T::V, row_on ? a.D : 0);
+    }
     const unsigned char* kbase = static_cast<const unsigned char*>(a.k.p) + ((long long)b * a.k.b + (long long)hk * a.k.h) * T::ES;
     const unsigned char* vbase = static_cast<const unsigned char*>(a.v.p) + ((long long)b * a.v.b + (long long)hk * a.v.h) * T::ES;
     const int len = key_count(a, b), tiles = (len + T::ROWS - 1) / T::ROWS;
@@ -117,12 +123,6 @@ attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int tot
     using Stream = AttnStream<E, DP>;
     const typename Stream::Map map(tid, a.D);
     Stream sk(map, kbase, t0 * T::ROWS, a.k.s), sv(map, vbase, t0 * T::ROWS, a.v.s);
-    u32x4_t fq[T::KS];
-    auto load_rows = [&] {
-        const unsigned char* qrow = row_on ? rows.at(a.q, G, b, hk, r, T::ES) : nullptr;
-#pragma unroll
-        for (int ks = 0; ks < T::KS; ++ks) fq[ks] = load_channels<E>(qrow, (2 * ks + half) * T::V, row_on ? a.D : 0);
-    };
     AttnState<E, DP> st;
     const float c2 = a.scale * kLog2e;
     auto valid = [&](int t) { return t < t1 ? valid_keys(a, b, t * T::ROWS, len) : 0ull; };
@@ -152,7 +152,6 @@ attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int tot
             sk.fetch(map, on);
             sv.fetch(map, on);
         }
-        load_rows();
         for (int t = t0; t < t1; ++t) {
             unsigned char* tk = lds + ((t - t0) & 1) * 2 * T::BYTES;
             unsigned char* tv = tk + T::BYTES;
@@ -170,7 +169,6 @@ attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int tot
     } else {
         unsigned char* tk = lds;
         unsigned char* tv = lds + T::BYTES;
-        load_rows();
         for (int t = t0; t < t1; ++t) {
             const unsigned long long on = valid(t);
             sk.fetch(map, on);

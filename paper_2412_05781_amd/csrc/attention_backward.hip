@@ -133,7 +133,7 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
         }
 #pragma unroll
         for (int q = 0; q < 16; ++q) {
-            dp[q] = s[q] == 0.f ? 0.f : s[q] * (dp[q] - dlt);
+            dp[q] = s[q] * (dp[q] - dlt);
             if constexpr (MEAN) rest += dp[q];
         }
 #pragma unroll

@@ -6,26 +6,13 @@
 // operand of the next product as they stand, if the other operand takes the streamed rows in the same order: element j of half h of step t is row
 // 16 t + 8 (j / 4) + 4 h + j % 4 for two-byte types, 8 t + 4 h + j for fp32.  Nothing is exchanged between lanes or passed through LDS.
 #pragma once
-#include "block_internal.h"
+#include "block_act.h"
 #include "wino_mma.h"
 
 namespace wino {
 
 typedef short attn_s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) attn_s16x4_t attn_lds_s16x4_t;
-
-// two neighbouring weights or results in one word, rounded to nearest even (one instruction, where two conversions and a merge take four)
-template <typename E> __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    const f32x2 v = {a, b};
-    if constexpr (std::is_same_v<E, bf16_t>) {
-        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-    } else {
-        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
-    }
-}
 
 // DP: channels / 16, rounded up
 template <typename E, int DP> struct AttnTile {

@@ -338,28 +338,25 @@ bool gemm_dims_ok(long long M, long long N, long long K) {
 // one row of sums per 32 rows, per 64 rows twice, per 128 rows twice or four times, or per 256 rows four times
 int gemm_most_sum_rows(int M) { return (M + 63) / 64 * 2 + 4; }
 
-// How many ranges a reduction is cut into.  Two-byte types: where there are fewer 64x64 tiles than the chip holds, down to ranges of sixteen stages (about
-// 5 us), which are worth the join.  fp32 is bound by its MFMAs, 0.49 us a stage of a 64x64 tile and compute unit, and what counts is how evenly the tiles
-// fill the units: the number with the least time in rounds of workgroups, the join's traffic counted (2028 x 2560 x 640, 320 tiles: one range
-// 88 us, two 76, four 72 with a join of single loads).
+// How many ranges a reduction is cut into: the number with the least time by this count.  A stage of a 64x64 tile takes a workgroup 0.29 us where it waits
+// for its operands (two-byte types, up to 768 workgroups side by side: 512 x 5120 x 1280, 160 tiles, 23 us) and 0.49 us of a compute unit's MFMAs for
+// fp32, where what counts is how evenly the tiles fill the units (2028 x 2560 x 640, 320 tiles: one range 88 us, four 70).  A join is 5 us and the
+// ranges' sums written and read.  Two-byte products with enough tiles of 128x128 are not cut at all.
 int gemm_ranges(int M, int N, int K, int dt) {
     auto tiles = [&](int n, int m) { return (((long long)N + n - 1) / n) * (((long long)M + m - 1) / m); };
+    const bool f32 = dt == DT_F32;
+    if (!f32 && tiles(128, 128) >= 130) return 1;
     const long long t64 = tiles(64, 64);
-    if (dt == DT_F32) {
-        const int stages = (K + 31) / 32;
-        int best = 1;
-        double least = 0.;
-        for (int n = 1; n <= 8 && (n == 1 || stages / n >= 8); ++n) {
-            const double us = 0.49 * (double)((t64 * n + 255) / 256) * ((stages + n - 1) / n) + (n == 1 ? 0. : 4. + (double)n * M * N * 8. / 4e6);
-            if (n == 1 || us < least) { best = n; least = us; }
-        }
-        return best;
+    const int stages = (K + (f32 ? 31 : 63)) / (f32 ? 32 : 64);
+    int best = 1;
+    double least = 0.;
+    for (int n = 1; n <= 16 && (n == 1 || stages / n >= 8); ++n) {
+        const double wide = (double)(t64 * n) / 768.;
+        const double us = (f32 ? 0.49 * (double)((t64 * n + 255) / 256) : 0.29 * (wide > 1. ? wide : 1.)) * ((stages + n - 1) / n) +
+                          (n == 1 ? 0. : 5. + (double)n * M * N * 8. / 4e6);
+        if (n == 1 || us < least) { best = n; least = us; }
     }
-    if (tiles(128, 128) >= 130) return 1;
-    long long n = 768 / t64;
-    if (n > K / 64 / 16) n = K / 64 / 16;
-    if (n > 16) n = 16;
-    return n < 2 ? 1 : (int)n;
+    return best;
 }
 
 hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, int dt, hipStream_t s,

@@ -81,7 +81,7 @@ template <typename E> __device__ __forceinline__ void load4(const E* p, int n, b
 template <typename E> __device__ __forceinline__ void store4(E* p, int n, bool whole, const float* v) {
     if (whole && n >= 4) {
         if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-        else *reinterpret_cast<uint2*>(p) = make_uint2(pack2<E>(v[0], v[1]), pack2<E>(v[2], v[3]));
+        else *reinterpret_cast<uint2*>(p) = make_uint2(pack_pair<E>(v[0], v[1]), pack_pair<E>(v[2], v[3]));
         return;
     }
 #pragma unroll

@@ -50,7 +50,7 @@ template <typename E> __device__ __forceinline__ void store8(E* p, const float* 
         reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
         reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
     } else {
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack2<E>(v[0], v[1]), pack2<E>(v[2], v[3]), pack2<E>(v[4], v[5]), pack2<E>(v[6], v[7]));
+        *reinterpret_cast<uint4*>(p) = make_uint4(pack_pair<E>(v[0], v[1]), pack_pair<E>(v[2], v[3]), pack_pair<E>(v[4], v[5]), pack_pair<E>(v[6], v[7]));
     }
 }
 
