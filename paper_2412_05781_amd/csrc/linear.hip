@@ -13,23 +13,23 @@ namespace {
 
 // four columns n0.. of row m, from the sums of one lane; returns in c (and c2: the gate half) what the column sums take
 template <typename E, int EP, int ACT>
-__device__ __forceinline__ void finish4(const GemmShape& g, const Epilogue& e, long long m, int n0, const float* s, const float* s2, bool whole, float* c, float* c2) {
+__device__ __forceinline__ void finish4(const GemmShape& g, const Epilogue& e, long long m, int n0, const float* s, const float* s2, float* c, float* c2) {
     const int n = g.N - n0;
     float a[4];
     if constexpr (EP == EP_STORE) {
-        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, whole, s);
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, s);
     } else if constexpr (EP == EP_LINEAR) {
         float r[4] = {0.f, 0.f, 0.f, 0.f};
-        if (e.extra) load4<E>(static_cast<const E*>(e.extra) + m * e.ld_extra + n0, n, whole, r);
+        if (e.extra) load4<E>(static_cast<const E*>(e.extra) + m * e.ld_extra + n0, n, r);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float b = e.bias && i < n ? e.bias[n0 + i] : 0.f;
             a[i] = act_only<E, ACT>(s[i] + b) + r[i];
         }
-        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, whole, a);
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, a);
     } else if constexpr (EP == EP_DLINEAR) {
         float r[4];
-        load4<E>(static_cast<const E*>(e.extra) + m * e.ld_extra + n0, n, whole, r);
+        load4<E>(static_cast<const E*>(e.extra) + m * e.ld_extra + n0, n, r);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float b = e.bias && i < n ? e.bias[n0 + i] : 0.f;
@@ -37,17 +37,17 @@ __device__ __forceinline__ void finish4(const GemmShape& g, const Epilogue& e, l
             act_both<E, ACT>(s[i] + b, v, d);
             c[i] = i < n ? r[i] * d : 0.f;
         }
-        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, whole, c);
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, c);
     } else if constexpr (EP == EP_GLU) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float bu = e.bias && i < n ? e.bias[n0 + i] : 0.f, bg = e.bias && i < n ? e.bias[g.N + n0 + i] : 0.f;
             a[i] = (s[i] + bu) * act_only<E, ACT>(s2[i] + bg);
         }
-        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, whole, a);
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, a);
     } else if constexpr (EP == EP_DGLU) {
         float r[4];
-        load4<E>(static_cast<const E*>(e.extra) + m * e.ld_extra + n0, n, whole, r);
+        load4<E>(static_cast<const E*>(e.extra) + m * e.ld_extra + n0, n, r);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float bu = e.bias && i < n ? e.bias[n0 + i] : 0.f, bg = e.bias && i < n ? e.bias[g.N + n0 + i] : 0.f;
@@ -56,17 +56,9 @@ __device__ __forceinline__ void finish4(const GemmShape& g, const Epilogue& e, l
             c[i] = i < n ? r[i] * v : 0.f;
             c2[i] = i < n ? r[i] * (s[i] + bu) * d : 0.f;
         }
-        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, whole, c);
-        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + g.N + n0, n, whole, c2);
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, c);
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + g.N + n0, n, c2);
     }
-}
-
-// whether rows of four neighbouring elements can be read and written as one access
-template <typename E> __device__ __forceinline__ bool rows_whole(const GemmShape& g, const Epilogue& e) {
-    constexpr int A = 4 * (int)sizeof(E);
-    uintptr_t bits = reinterpret_cast<uintptr_t>(e.out) | (uintptr_t)(e.ld_out * (long long)sizeof(E)) | (uintptr_t)(g.N * (int)sizeof(E));
-    if (e.extra) bits |= reinterpret_cast<uintptr_t>(e.extra) | (uintptr_t)(e.ld_extra * (long long)sizeof(E));
-    return (bits & (A - 1)) == 0;
 }
 
 __device__ __forceinline__ float sum_over_32(float v) {
@@ -75,12 +67,12 @@ __device__ __forceinline__ float sum_over_32(float v) {
     return v;
 }
 
-// ---- the kernel for every shape: operands go through registers, element by element where alignment or the edge asks for it -------------------
+// ---- the kernel for every shape: operands go through registers, at any alignment, element by element at the edge -------------------
 constexpr int kBP = 128, kBQ = 64;       // tile: 128 rows of P x 64 rows of Q, four waves, 64 x 32 each
 
 template <typename E, int EP, int ACT, bool PA, bool QA>
 __global__ void __launch_bounds__(256) gemm_any_kernel(Operand P, Operand Q, GemmShape g, Epilogue e, int tiles_p, int tiles_q, int total, int per_xcd,
-                                                       int nsplit, bool p_vec, bool q_vec) {
+                                                       int nsplit) {
     constexpr bool GLU = EP == EP_GLU || EP == EP_DGLU;
     constexpr int BK = 128 / (int)sizeof(E), V = 16 / (int)sizeof(E);
     constexpr int P_CHUNKS = kBP * 8 / 256, Q_CHUNKS = kBQ * 8 / 256;
@@ -114,12 +106,12 @@ __global__ void __launch_bounds__(256) gemm_any_kernel(Operand P, Operand Q, Gem
             if constexpr (!PA) {
                 const int r = id >> 3, k = k0 + (id & 7) * V, n = p_left(r) > 0 ? g.K - k : 0;
                 const E* at = pp + (long long)p_row(r) * P.ld + k;
-                rp[i] = n <= 0 ? zero : p_vec && n >= V ? *reinterpret_cast<const u32x4_t*>(at) : load_part<E>(at, n);
+                rp[i] = n <= 0 ? zero : load_part<E>(at, n);
             } else {
                 constexpr int CPR = kBP / V;
                 const int k = k0 + id / CPR, r = (id % CPR) * V, n = k < g.K ? p_left(r) : 0;
                 const E* at = pp + (long long)k * P.ld + p_row(r);
-                rp[i] = n <= 0 ? zero : p_vec && n >= V ? *reinterpret_cast<const u32x4_t*>(at) : load_part<E>(at, n);
+                rp[i] = n <= 0 ? zero : load_part<E>(at, n);
             }
         }
 #pragma unroll
@@ -130,7 +122,7 @@ __global__ void __launch_bounds__(256) gemm_any_kernel(Operand P, Operand Q, Gem
                 const long long m = m0 + (id >> 3);
                 const int n = m < g.M ? g.K - k : 0;
                 const E* at = qp + m * Q.ld + k;
-                rq[i] = n <= 0 ? zero : q_vec && n >= V ? *reinterpret_cast<const u32x4_t*>(at) : load_part<E>(at, n);
+                rq[i] = n <= 0 ? zero : load_part<E>(at, n);
             } else {
                 constexpr int CPR = kBQ / V;
                 const int k = k0 + id / CPR;
@@ -138,7 +130,7 @@ __global__ void __launch_bounds__(256) gemm_any_kernel(Operand P, Operand Q, Gem
                 const long long left = k < g.K ? g.M - m : 0;
                 const int n = left > V ? V : (int)left;
                 const E* at = qp + (long long)k * Q.ld + m;
-                rq[i] = n <= 0 ? zero : q_vec && n >= V ? *reinterpret_cast<const u32x4_t*>(at) : load_part<E>(at, n);
+                rq[i] = n <= 0 ? zero : load_part<E>(at, n);
             }
         }
     };
@@ -189,7 +181,6 @@ __global__ void __launch_bounds__(256) gemm_any_kernel(Operand P, Operand Q, Gem
             }
         return;
     }
-    const bool whole = rows_whole<E>(g, e);
     constexpr bool SUMS = EP == EP_DLINEAR || EP == EP_DGLU;
 #pragma unroll
     for (int i = 0; i < (GLU ? 1 : 2); ++i)
@@ -199,7 +190,7 @@ __global__ void __launch_bounds__(256) gemm_any_kernel(Operand P, Operand Q, Gem
             float s[4], s2[4], c[4] = {}, c2[4] = {};
 #pragma unroll
             for (int j = 0; j < 4; ++j) { s[j] = acc[i][4 * q + j]; s2[j] = acc[1][4 * q + j]; }
-            if (m < g.M && n < g.N) finish4<E, EP, ACT>(g, e, m, n, s, s2, whole, c, c2);
+            if (m < g.M && n < g.N) finish4<E, EP, ACT>(g, e, m, n, s, s2, c, c2);
             if constexpr (SUMS) {
                 const long long row = (long long)bq * 2 + wq;
                 const int width = EP == EP_DGLU ? 2 * g.N : g.N;
@@ -223,10 +214,8 @@ hipError_t launch_any(const Operand& P, const Operand& Q, const GemmShape& g, co
     const long long tp = (g.N + bn - 1) / bn, tq = ((long long)g.M + kBQ - 1) / kBQ, total = tp * tq * nsplit;
     if (total > 0x3fffffffLL) return hipErrorInvalidValue;
     const int per_xcd = (int)((total + 7) / 8);
-    // the gate half of a transposed P starts at column N
-    const bool p_vec = vec_rows<E>(P) && !(GLU && PA && (g.N * sizeof(E)) % 16 != 0);
     hipLaunchKernelGGL((gemm_any_kernel<E, EP, ACT, PA, QA>), dim3((unsigned)(per_xcd * 8)), dim3(256), 0, s, P, Q, g, e, (int)tp, (int)tq, (int)total, per_xcd,
-                       nsplit, p_vec, vec_rows<E>(Q));
+                       nsplit);
     return hipGetLastError();
 }
 
@@ -268,9 +257,8 @@ template <typename E, int ACT> __global__ void __launch_bounds__(256) join_kerne
             for (int i = 0; i < 4; ++i)
                 if (n0 + i < g.N) s[i] += p[(size_t)r * step + i];
     }
-    const bool whole = rows_whole<E>(g, e);
-    if (linear) finish4<E, EP_LINEAR, ACT>(g, e, m, n0, s, s, whole, nullptr, nullptr);
-    else finish4<E, EP_STORE, ACT>(g, e, m, n0, s, s, whole, nullptr, nullptr);
+    if (linear) finish4<E, EP_LINEAR, ACT>(g, e, m, n0, s, s, nullptr, nullptr);
+    else finish4<E, EP_STORE, ACT>(g, e, m, n0, s, s, nullptr, nullptr);
 }
 
 // 64 columns per workgroup, sixteen waves that take every sixteenth row

@@ -21,7 +21,7 @@ template <typename E> __device__ __forceinline__ void mma16(const u32x4_t& a, co
 
 // MT tiles of 16 rows of x
 template <typename E, bool GLU, int MT>
-__global__ void __launch_bounds__(kWaves * 64) gemm_few_kernel(Operand P, Operand Q, GemmShape g, Epilogue e, bool vec) {
+__global__ void __launch_bounds__(kWaves * 64) gemm_few_kernel(Operand P, Operand Q, GemmShape g, Epilogue e) {
     constexpr int V = 16 / (int)sizeof(E), NW = GLU ? 2 : 1, U = MT * NW > 4 ? 2 : 4, TILES = MT * NW, ROW = 20;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n0 = blockIdx.x * kCols, idx = lane & 15, quarter = lane >> 4;
@@ -41,10 +41,10 @@ __global__ void __launch_bounds__(kWaves * 64) gemm_few_kernel(Operand P, Operan
         const u32x4_t zero = {0, 0, 0, 0};
         const int left = on ? g.K - k : 0;
         if (left <= 0) return zero;
-        return vec && left >= V ? *reinterpret_cast<const u32x4_t*>(row + k) : load_part<E>(row + k, left);
+        return load_part<E>(row + k, left);
     };
     // rows behind the edge repeat row 0: their sums are not stored
-    const int full = vec ? g.K / (4 * V) : 0;              // steps that need no guard
+    const int full = g.K / (4 * V);                        // steps that need no guard
     int s = wave;
     for (; s + kWaves * (U - 1) < full; s += kWaves * U) {
         u32x4_t fw[U][NW], fx[U][MT];
@@ -52,9 +52,9 @@ __global__ void __launch_bounds__(kWaves * 64) gemm_few_kernel(Operand P, Operan
         for (int u = 0; u < U; ++u) {
             const int k = (s + kWaves * u) * 4 * V + quarter * V;
 #pragma unroll
-            for (int h = 0; h < NW; ++h) fw[u][h] = *reinterpret_cast<const u32x4_t*>(wrow[h] + k);
+            for (int h = 0; h < NW; ++h) fw[u][h] = load_part<E>(wrow[h] + k, V);
 #pragma unroll
-            for (int t = 0; t < MT; ++t) fx[u][t] = *reinterpret_cast<const u32x4_t*>(xrow[t] + k);
+            for (int t = 0; t < MT; ++t) fx[u][t] = load_part<E>(xrow[t] + k, V);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -113,7 +113,7 @@ template <typename E, bool GLU, int MT> hipError_t launch_few(const Operand& P, 
     auto kern = gemm_few_kernel<E, GLU, MT>;
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((g.N + kCols - 1) / kCols)), dim3(kWaves * 64), bytes, s, P, Q, g, e, vec_rows<E>(P) && vec_rows<E>(Q));
+    hipLaunchKernelGGL(kern, dim3((unsigned)((g.N + kCols - 1) / kCols)), dim3(kWaves * 64), bytes, s, P, Q, g, e);
     return hipGetLastError();
 }
 

@@ -49,10 +49,14 @@ template <typename E, bool ACROSS, int BI> __device__ __forceinline__ u32x4_t re
     }
 }
 
-// n elements (up to 16 bytes) from p, the rest zero
+// n elements (up to 16 bytes) from p, the rest zero.  Whole chunks are one load at any alignment of the elements.
 template <typename E> __device__ __forceinline__ u32x4_t load_part(const E* p, int n) {
     u32x4_t f = {0, 0, 0, 0};
     constexpr int V = 16 / (int)sizeof(E);
+    if (n >= V) {
+        __builtin_memcpy(&f, p, 16);
+        return f;
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         if (i < n) {
@@ -63,14 +67,14 @@ template <typename E> __device__ __forceinline__ u32x4_t load_part(const E* p, i
     return f;
 }
 
-// four neighbouring elements of a row: as one access where every row allows it
-template <typename E> __device__ __forceinline__ void load4(const E* p, int n, bool whole, float* v) {
-    if (whole && n >= 4) {
+// four neighbouring elements of a row, one access at any alignment of the elements
+template <typename E> __device__ __forceinline__ void load4(const E* p, int n, float* v) {
+    if (n >= 4) {
         if constexpr (sizeof(E) == 4) {
-            const float4 f = *reinterpret_cast<const float4*>(p);
-            v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+            __builtin_memcpy(v, p, 16);
         } else {
-            const uint2 f = *reinterpret_cast<const uint2*>(p);
+            uint2 f;
+            __builtin_memcpy(&f, p, 8);
             v[0] = lo16<E>(f.x); v[1] = hi16<E>(f.x); v[2] = lo16<E>(f.y); v[3] = hi16<E>(f.y);
         }
         return;
@@ -78,10 +82,14 @@ template <typename E> __device__ __forceinline__ void load4(const E* p, int n, b
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = i < n ? to_f32<E>(p[i]) : 0.f;
 }
-template <typename E> __device__ __forceinline__ void store4(E* p, int n, bool whole, const float* v) {
-    if (whole && n >= 4) {
-        if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-        else *reinterpret_cast<uint2*>(p) = make_uint2(pack_pair<E>(v[0], v[1]), pack_pair<E>(v[2], v[3]));
+template <typename E> __device__ __forceinline__ void store4(E* p, int n, const float* v) {
+    if (n >= 4) {
+        if constexpr (sizeof(E) == 4) {
+            __builtin_memcpy(p, v, 16);
+        } else {
+            const uint2 f = make_uint2(pack_pair<E>(v[0], v[1]), pack_pair<E>(v[2], v[3]));
+            __builtin_memcpy(p, &f, 8);
+        }
         return;
     }
 #pragma unroll
