@@ -373,27 +373,38 @@ template <typename E> __global__ void __launch_bounds__(256) attention_join_kern
 // Whether the rows of a key head fit one wave's tile.
 bool few_rows(int Sq, int H, int Hkv) { return (long long)(H / Hkv) * Sq <= 32; }
 
-// Ranges of the keys, where the rows alone leave compute units idle: about two workgroups a unit (few rows: four, because lengths that differ leave
-// some of them short), at least 256 keys a range (few rows: 128 a wave).
-int attention_ranges(int B, int Sq, int Skv, int H, int Hkv) {
-    const bool few = few_rows(Sq, H, Hkv);
-    const long long blocks = few ? (long long)B * Hkv : (long long)B * Hkv * (((long long)(H / Hkv) * Sq + 127) / 128);
-    long long n = (few ? 1024 : 512) / blocks;
-    const int most = Skv / (few ? 512 : 256);
-    if (n > most) n = most;
-    if (n > 64) n = 64;
-    return n < 2 ? 1 : (int)n;
+// Ranges of the keys, where the rows alone leave compute units idle.  Few rows: about four workgroups a unit, because lengths that differ leave some of
+// them short, and at least 128 keys a wave.  Otherwise the number with the least time by this count: 1 us a tile of keys for up to two workgroups
+// a unit (fp32: its MFMAs, 0.06 us a channel); a join is 5 us and the parts written and read (16 heads x 1024 x 1024 x 80 in fp16, 128 workgroups: one
+// range 31, four 45 us).
+int attention_ranges(int B, int Sq, int Skv, int H, int Hkv, int D, int dt) {
+    if (few_rows(Sq, H, Hkv)) {
+        long long n = 1024 / ((long long)B * Hkv);
+        if (n > Skv / 512) n = Skv / 512;
+        if (n > 64) n = 64;
+        return n < 2 ? 1 : (int)n;
+    }
+    const long long blocks = (long long)B * Hkv * (((long long)(H / Hkv) * Sq + 127) / 128);
+    const int tiles = (Skv + 63) / 64;
+    int best = 1;
+    double least = 0.;
+    for (int n = 1; n <= 64 && (n == 1 || tiles / n >= 4); ++n) {
+        const double wide = (double)(blocks * n) / 512.;
+        const double us = (dt == DT_F32 ? 1. + 0.06 * D : 1.) * (double)((tiles + n - 1) / n) * (wide > 1. ? wide : 1.) + (n == 1 ? 0. : 5. + (double)n * B * H * Sq * D * 8. / 4e6);
+        if (n == 1 || us < least) { best = n; least = us; }
+    }
+    return best;
 }
 
 }  // namespace
 
-size_t attention_ws_bytes(int B, int Sq, int Skv, int H, int Hkv, int D, int) {
-    const int n = attention_ranges(B, Sq, Skv, H, Hkv);
+size_t attention_ws_bytes(int B, int Sq, int Skv, int H, int Hkv, int D, int dt) {
+    const int n = attention_ranges(B, Sq, Skv, H, Hkv, D, dt);
     return n == 1 ? 0 : (size_t)n * B * H * Sq * ((size_t)D + 1) * sizeof(float);
 }
 
 hipError_t launch_attention(const AttnArgs& a, int dt, hipStream_t s) {
-    const int R = a.H / a.Hkv * a.Sq, nsplit = attention_ranges(a.B, a.Sq, a.Skv, a.H, a.Hkv), row_tiles = (R + 127) / 128;
+    const int R = a.H / a.Hkv * a.Sq, nsplit = attention_ranges(a.B, a.Sq, a.Skv, a.H, a.Hkv, a.D, dt), row_tiles = (R + 127) / 128;
     const long long all = (long long)a.B * a.Hkv * R, total = (long long)a.B * a.Hkv * row_tiles * nsplit;
     if (total > 0x3fffffffLL || all > 0x7fffffffLL) return hipErrorInvalidValue;
     const int per_xcd = (int)((total + 7) / 8);

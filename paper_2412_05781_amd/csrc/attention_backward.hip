@@ -333,26 +333,31 @@ template <typename E> __global__ void __launch_bounds__(256) attention_dkv_join_
     store_channels<E>(static_cast<unsigned char*>(const_cast<void*>(a.dv.p)) + ((long long)b * a.dv.b + (long long)hk * a.dv.h + (long long)key * a.dv.s) * ES, c, a.D, y);
 }
 
-// Ranges of the query rows, where the keys alone leave compute units idle: about two workgroups a unit, at least four tiles of rows a range.
-int backward_ranges(int B, int Sq, int Skv, int H, int Hkv) {
+// Ranges of the query rows, where the keys alone leave compute units idle: the number with the least time by this count, 1.3 us a tile of rows for up to
+// two workgroups a unit (fp32: its MFMAs, 0.06 us a channel more); a join is 5 us and the parts written and read.
+int backward_ranges(int B, int Sq, int Skv, int H, int Hkv, int D, int dt) {
     const long long blocks = (long long)B * Hkv * (((long long)Skv + 63) / 64);
     const long long tiles = (long long)(H / Hkv) * ((Sq + 63) / 64);
-    long long n = 512 / blocks;
-    if (n > tiles / 4) n = tiles / 4;
-    if (n > 16) n = 16;
-    return n < 2 ? 1 : (int)n;
+    int best = 1;
+    double least = 0.;
+    for (int n = 1; n <= 16 && (n == 1 || tiles / n >= 4); ++n) {
+        const double wide = (double)(blocks * n) / 512.;
+        const double us = (dt == DT_F32 ? 1.3 + 0.06 * D : 1.3) * (double)((tiles + n - 1) / n) * (wide > 1. ? wide : 1.) + (n == 1 ? 0. : 5. + (double)n * B * Hkv * Skv * D * 16. / 4e6);
+        if (n == 1 || us < least) { best = n; least = us; }
+    }
+    return best;
 }
 size_t align_floats(size_t n) { return (n + 63) / 64 * 64; }
 
 }  // namespace
 
-size_t attention_backward_ws_bytes(int B, int Sq, int Skv, int H, int Hkv, int D, int) {
-    const int n = backward_ranges(B, Sq, Skv, H, Hkv);
+size_t attention_backward_ws_bytes(int B, int Sq, int Skv, int H, int Hkv, int D, int dt) {
+    const int n = backward_ranges(B, Sq, Skv, H, Hkv, D, dt);
     return (align_floats((size_t)B * H * Sq) + (n == 1 ? 0 : 2 * (size_t)n * B * Hkv * Skv * D)) * sizeof(float);
 }
 
 hipError_t launch_attention_backward(const AttnArgs& a, int dt, hipStream_t s) {
-    const int R = a.H / a.Hkv * a.Sq, nsplit = backward_ranges(a.B, a.Sq, a.Skv, a.H, a.Hkv);
+    const int R = a.H / a.Hkv * a.Sq, nsplit = backward_ranges(a.B, a.Sq, a.Skv, a.H, a.Hkv, a.D, dt);
     const int row_tiles = (R + 63) / 64, key_tiles = (a.Skv + 63) / 64;
     const long long all = (long long)a.B * a.Hkv * R, qt = (long long)a.B * a.Hkv * row_tiles, kt = (long long)a.B * a.Hkv * key_tiles * nsplit;
     const long long joins = ((long long)a.B * a.Hkv * a.Skv * (a.D / 4) + 255) / 256;
