@@ -107,6 +107,7 @@ attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int tot
     const int b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
     const AttnRows rows{a.Sq, G * a.Sq};
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const typename T::Places places(lane);
     const int r = tile * 128 + wave * 32 + (lane & 31);
     const bool row_on = r < rows.R;
 
@@ -131,7 +132,7 @@ attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int tot
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int ks = 0; ks < T::KS; ++ks) Mma<E>::run(T::along(tk, 32 * i, ks, lane), fq[ks], s[i]);
+            for (int ks = 0; ks < T::KS; ++ks) Mma<E>::run(T::along(tk, 32 * i, ks, places), fq[ks], s[i]);
         st.template settle<2>(s, on, half, c2);
         const float sh = st.shift();
 #pragma unroll
@@ -141,7 +142,7 @@ attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int tot
             for (int k = 0; k < T::ST; ++k) {
                 const u32x4_t w = T::weights(s[i], k);
 #pragma unroll
-                for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(tv, 32 * i, k, d, lane), w, st.acc[d]);
+                for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(tv, 32 * i, k, d, places), w, st.acc[d]);
             }
         }
     };
@@ -206,6 +207,7 @@ attention_few_kernel(AttnArgs a, AttnParts parts, int nsplit) {
     const int b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
     const AttnRows rows{a.Sq, G * a.Sq};
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const typename T::Places places(lane);
     const int r = lane & 31;
     const bool row_on = r < rows.R;
     unsigned char* tk = lds + wave * F::WAVE_BYTES;
@@ -275,7 +277,7 @@ attention_few_kernel(AttnArgs a, AttnParts parts, int nsplit) {
 #pragma unroll
         for (int i = 0; i < F::SUBS; ++i)
 #pragma unroll
-            for (int ks = 0; ks < T::KS; ++ks) Mma<E>::run(T::along(tk, 32 * i, ks, lane), fq[ks], s[i]);
+            for (int ks = 0; ks < T::KS; ++ks) Mma<E>::run(T::along(tk, 32 * i, ks, places), fq[ks], s[i]);
         st.template settle<F::SUBS>(s, cur, half, c2);
         const float sh = st.shift();
 #pragma unroll
@@ -285,7 +287,7 @@ attention_few_kernel(AttnArgs a, AttnParts parts, int nsplit) {
             for (int k = 0; k < T::ST; ++k) {
                 const u32x4_t w = T::weights(s[i], k);
 #pragma unroll
-                for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(tv, 32 * i, k, d, lane), w, st.acc[d]);
+                for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(tv, 32 * i, k, d, places), w, st.acc[d]);
             }
         }
     }

@@ -55,6 +55,7 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
     const int slot = logical / row_tiles, tile = logical - slot * row_tiles, bh = deal_heads(slot, a.B * a.Hkv), b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
     const AttnRows rows{a.Sq, G * a.Sq};
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, sub = wave >> 1;
+    const typename T::Places places(lane);
     const int r = tile * 64 + (wave & 1) * 32 + (lane & 31);
     const bool row_on = r < rows.R;
     const unsigned char* kbase = static_cast<const unsigned char*>(a.k.p) + ((long long)b * a.k.b + (long long)hk * a.k.h) * T::ES;
@@ -119,8 +120,8 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
         float16_t s = {}, dp = {};
 #pragma unroll
         for (int ks = 0; ks < T::KS; ++ks) {
-            Mma<E>::run(T::along(tk, 32 * sub, ks, lane), fq[ks], s);
-            Mma<E>::run(T::along(tv, 32 * sub, ks, lane), fo[ks], dp);
+            Mma<E>::run(T::along(tk, 32 * sub, ks, places), fq[ks], s);
+            Mma<E>::run(T::along(tv, 32 * sub, ks, places), fo[ks], dp);
         }
 #pragma unroll
         for (int q = 0; q < 16; ++q) s[q] = __builtin_amdgcn_exp2f(fmaf(s[q], c2, -lse2));
@@ -141,7 +142,7 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
             const u32x4_t w = T::weights(dp, st), wp = MEAN ? T::weights(s, st) : w;
 #pragma unroll
             for (int d = 0; d < T::NV; ++d) {
-                const u32x4_t keys = T::across(tk, 32 * sub, st, d, lane);
+                const u32x4_t keys = T::across(tk, 32 * sub, st, d, places);
                 Mma<E>::run(keys, w, acc[d]);
                 if constexpr (MEAN) Mma<E>::run(keys, wp, acc[T::NV + d]);
             }
@@ -187,6 +188,7 @@ attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit,
     const int bh = deal_heads(slot, a.B * a.Hkv);
     const int b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, sub = wave >> 1;
+    const typename T::Places places(lane);
     const int len = key_count(a, b), key = tile * 64 + (wave & 1) * 32 + (lane & 31);
     const bool in_range = key < a.Skv, key_on = key < len && (!a.key_mask || a.key_mask[(long long)b * a.Skv + key] != 0);
     // acc: dk, then dv.  What a lane whose key is not valid sums stays in its own column and is dropped at the end.
@@ -249,8 +251,8 @@ attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit,
             float16_t s = {}, dp = {};
 #pragma unroll
             for (int ks = 0; ks < T::KS; ++ks) {
-                Mma<E>::run(T::along(tq, 32 * sub, ks, lane), fk[ks], s);
-                Mma<E>::run(T::along(to, 32 * sub, ks, lane), fv[ks], dp);
+                Mma<E>::run(T::along(tq, 32 * sub, ks, places), fk[ks], s);
+                Mma<E>::run(T::along(to, 32 * sub, ks, places), fv[ks], dp);
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -268,8 +270,8 @@ attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit,
                 const u32x4_t wp = T::weights(s, st), wd = T::weights(dp, st);
 #pragma unroll
                 for (int d = 0; d < T::NV; ++d) {
-                    Mma<E>::run(T::across(to, 32 * sub, st, d, lane), wp, acc[T::NV + d]);
-                    Mma<E>::run(T::across(tq, 32 * sub, st, d, lane), wd, acc[d]);
+                    Mma<E>::run(T::across(to, 32 * sub, st, d, places), wp, acc[T::NV + d]);
+                    Mma<E>::run(T::across(tq, 32 * sub, st, d, places), wd, acc[d]);
                 }
             }
         }

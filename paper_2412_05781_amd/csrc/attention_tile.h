@@ -32,28 +32,44 @@ template <typename E, int DP> struct AttnTile {
     static __device__ __forceinline__ int at(int row, int chunk) {
         return row * STRIDE + ((ES == 2 ? chunk ^ ((row >> 2) & 3) : chunk) << 4);
     }
-    // row row0 + lane % 32, channels of step ks
-    static __device__ __forceinline__ u32x4_t along(const unsigned char* t, int row0, int ks, int lane) {
-        return *reinterpret_cast<const u32x4_t*>(t + at(row0 + (lane & 31), 2 * ks + (lane >> 5)));
-    }
-    // channel 32 dt + lane % 32, rows of step st from row0
-    static __device__ __forceinline__ u32x4_t across(const unsigned char* t, int row0, int st, int dt, int lane) {
-        const int half = lane >> 5;
-        u32x4_t f;
-        if constexpr (ES == 2) {
-            const int col = dt * 32 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    // Where a lane reads.  Rows start at multiples of 32 (two-byte types: or 16), which leave the flipped bits alone, so that a read is one of four places per
+    // lane and a constant: row lane % 32 along the channels (two-byte types: even and odd steps), or its rows and channel across.
+    struct Places {
+        int along[2], across[2];
+        __device__ __forceinline__ explicit Places(int lane) {
+            const int half = lane >> 5, row = lane & 31;
+            along[0] = at(row, half);
+            along[1] = at(row, 2 + half);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const int row = row0 + 16 * st + 8 * k + 4 * half + ((lane & 15) >> 2);
-                const attn_s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((attn_lds_s16x4_t*)(t + at(row, col >> 3) + ((col & 4) << 1)));
+                if constexpr (ES == 2) {                       // four rows x 16 channels per 16 lanes and read; lane i of the 16 gets channel i
+                    const int col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+                    across[k] = at(8 * k + 4 * half + ((lane & 15) >> 2), col >> 3) + ((col & 4) << 1);
+                } else {
+                    across[k] = at(4 * half, row >> 2) + ((row & 3) << 2);
+                }
+            }
+        }
+    };
+    // row row0 + lane % 32, channels of step ks
+    static __device__ __forceinline__ u32x4_t along(const unsigned char* t, int row0, int ks, const Places& p) {
+        const int place = ES == 2 ? p.along[ks & 1] + (ks >> 1) * 64 : p.along[0] + ks * 32;
+        return *reinterpret_cast<const u32x4_t*>(t + row0 * STRIDE + place);
+    }
+    // channel 32 dt + lane % 32, rows of step st from row0
+    static __device__ __forceinline__ u32x4_t across(const unsigned char* t, int row0, int st, int dt, const Places& p) {
+        u32x4_t f;
+        if constexpr (ES == 2) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const attn_s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((attn_lds_s16x4_t*)(t + (row0 + 16 * st) * STRIDE + p.across[k] + dt * 64));
                 const uint2 w = __builtin_bit_cast(uint2, v);
                 f[2 * k] = w.x;
                 f[2 * k + 1] = w.y;
             }
         } else {
-            const int col = dt * 32 + (lane & 31);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<const uint32_t*>(t + at(row0 + 8 * st + 4 * half + j, col >> 2) + ((col & 3) << 2));
+            for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<const uint32_t*>(t + (row0 + 8 * st + j) * STRIDE + p.across[0] + dt * 128);
         }
         return f;
     }
