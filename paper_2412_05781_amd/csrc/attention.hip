@@ -95,7 +95,7 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, const AttnParts& pa
 // Two waves a SIMD as long as their registers suffice; wide heads give up the tile on its way for that.
 template <typename E, int DP> constexpr int attention_waves() { return DP <= (sizeof(E) == 2 ? 10 : 5) ? 2 : 1; }
 template <typename E, int DP> constexpr int attention_few_waves() { return DP <= 4 ? 2 : 1; }
-template <typename E, int DP> constexpr bool attention_ahead() { return sizeof(E) == 2 && DP <= 6; }
+template <typename E, int DP> constexpr bool attention_ahead() { return sizeof(E) == 2 && DP <= 8; }
 template <typename E, int DP> __global__ void __launch_bounds__(256, (attention_waves<E, DP>()))
 attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int total, int per_xcd) {
     using T = AttnTile<E, DP>;
