@@ -651,7 +651,7 @@ def _on_one_device(stream, first, *others):
 
 def _rows(t: torch.Tensor, name: str, shape, dtype) -> int:
     """The row stride of a [rows, cols] tensor whose rows are contiguous."""
-    if t.shape != shape or t.dtype != dtype:
+    if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{name} must be {list(shape)} of {dtype}")
     ld, step = t.stride()
     if step != 1 and shape[1] > 1:
@@ -660,13 +660,13 @@ def _rows(t: torch.Tensor, name: str, shape, dtype) -> int:
 
 
 def _weights(x, w, bias, halves: int):
-    """(x's shape, N, dtype code) of x[M,K], w[halves*N,K] and bias[halves*N]."""
-    dt, xs, ws = DTYPE_OF.get(x.dtype), x.shape, w.shape
-    if dt is None or len(xs) != 2 or len(ws) != 2 or w.dtype != x.dtype or ws[1] != xs[1] or ws[0] % halves or not w.is_contiguous():
+    """(x's shape, rows of w per half, x's type, its code) of x[M,K], w[halves*N,K] and bias[halves*N]."""
+    xd, xs, ws = x.dtype, tuple(x.shape), w.shape
+    if xd not in DTYPE_OF or len(xs) != 2 or len(ws) != 2 or w.dtype is not xd or ws[1] != xs[1] or ws[0] % halves or not w.is_contiguous():
         raise ValueError("x must be [M, K] and w a contiguous [N, K] (gated: [2N, K]) of the same storage type")
-    if bias is not None and (bias.dtype != torch.float32 or bias.numel() != ws[0] or not bias.is_contiguous()):
+    if bias is not None and (bias.dtype is not torch.float32 or bias.numel() != ws[0] or not bias.is_contiguous()):
         raise ValueError("bias must be a contiguous fp32 tensor with one element per row of w")
-    return xs, ws[0] // halves, dt
+    return xs, ws[0] // halves, xd, DTYPE_OF[xd]
 
 
 def _ws(workspace):
@@ -674,7 +674,7 @@ def _ws(workspace):
         return None, 0
     if not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def wino_linear_workspace_bytes(M, N, K, dtype, act=WINO_ACT_NONE) -> int:
@@ -695,10 +695,11 @@ def wino_glu_backward_workspace_bytes(M, N, K, dtype, act) -> int:
 
 def wino_linear(x, w, bias, y, act: int = WINO_ACT_NONE, residual=None, workspace=None, stream=None):
     """y[M,N] = act(x[M,K] w[N,K]^T + bias) + residual; rows of x, y and residual may be strided, residual may be y."""
-    xs, N, dt = _weights(x, w, bias, 1)
+    xs, N, xd, dt = _weights(x, w, bias, 1)
     M, K = xs
-    ldx, ldy = _rows(x, "x", xs, x.dtype), _rows(y, "y", (M, N), x.dtype)
-    ldr = ldy if residual is None else _rows(residual, "residual", (M, N), x.dtype)
+    ys = M, N
+    ldx, ldy = _rows(x, "x", xs, xd), _rows(y, "y", ys, xd)
+    ldr = ldy if residual is None else _rows(residual, "residual", ys, xd)
     _on_one_device(stream, x, w, bias, y, residual, workspace)
     ws, n = _ws(workspace)
     _check(lib().wino_linear(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), y.data_ptr(), M, N, K, ldx, ldr, ldy, dt, act, ws, n,
@@ -707,10 +708,10 @@ def wino_linear(x, w, bias, y, act: int = WINO_ACT_NONE, residual=None, workspac
 
 
 def _product_backward(name, halves, x, w, bias, dy, dx, dw, dbias, act, workspace, stream):
-    xs, N, dt = _weights(x, w, bias, halves)
+    xs, N, xd, dt = _weights(x, w, bias, halves)
     M, K = xs
-    ldx, lddy = _rows(x, "x", xs, x.dtype), _rows(dy, "the output's gradient", (M, N), x.dtype)
-    lddx = K if dx is None else _rows(dx, "dx", xs, x.dtype)
+    ldx, lddy = _rows(x, "x", xs, xd), _rows(dy, "the output's gradient", (M, N), xd)
+    lddx = K if dx is None else _rows(dx, "dx", xs, xd)
     if dw is not None and (dw.shape != w.shape or dw.dtype != x.dtype or not dw.is_contiguous()):
         raise ValueError("dw must be contiguous with the shape and type of w")
     if dbias is not None and (dbias.dtype != torch.float32 or dbias.numel() != halves * N or not dbias.is_contiguous()):
@@ -729,9 +730,9 @@ def wino_linear_backward(x, w, bias, dy, dx, dw, dbias, act: int = WINO_ACT_NONE
 
 def wino_glu(x, w, bias, h, act: int = WINO_ACT_GELU, workspace=None, stream=None):
     """h[M,N] = (x wu^T + bu) * act(x wg^T + bg) with w[2N,K] = wu above wg and bias[2N] = bu, bg."""
-    xs, N, dt = _weights(x, w, bias, 2)
+    xs, N, xd, dt = _weights(x, w, bias, 2)
     M, K = xs
-    ldx, ldh = _rows(x, "x", xs, x.dtype), _rows(h, "h", (M, N), x.dtype)
+    ldx, ldh = _rows(x, "x", xs, xd), _rows(h, "h", (M, N), xd)
     _on_one_device(stream, x, w, bias, h, workspace)
     ws, n = _ws(workspace)
     _check(lib().wino_glu(x.data_ptr(), w.data_ptr(), _ptr(bias), h.data_ptr(), M, N, K, ldx, ldh, dt, act, ws, n, _stream(stream)), "wino_glu")
@@ -754,9 +755,9 @@ def wino_attention_backward_workspace_bytes(B, Sq, Skv, H, Hkv, D, dtype) -> int
 def _heads(t, name, shape, dtype):
     """(address, strides of batch, position and head): a wino_tensor"""
     st = t.stride()
-    if t.shape != shape or t.dtype != dtype or (st[-1] != 1 and shape[3] > 1):
+    if t.shape != shape or t.dtype is not dtype or (st[3] != 1 and shape[3] > 1):
         raise ValueError(f"{name} must be {list(shape)} of {dtype} with contiguous channels")
-    return t.data_ptr(), *st[:3]
+    return t.data_ptr(), st[0], st[1], st[2]
 
 
 _ATTENTION_ARGS = struct.Struct("@7if" + "Pqqq" * 4 + "PPP" + "Pqqq" * 4)        # wino_attention_args
@@ -764,7 +765,7 @@ _NO_GRADIENTS = (0,) * 16
 
 
 def _attention(q, k, v, o, lse, kv_len, key_mask, scale, gradients=None):
-    qs, ks, dtype = q.shape, k.shape, q.dtype
+    qs, ks, dtype = tuple(q.shape), k.shape, q.dtype
     if len(qs) != 4 or len(ks) != 4 or dtype not in DTYPE_OF:
         raise ValueError("q must be [B, Sq, H, D] and k, v [B, Skv, Hkv, D] in one of the storage types")
     B, Sq, H, D = qs
