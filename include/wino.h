@@ -385,6 +385,7 @@ typedef enum wino_act { WINO_ACT_NONE = 0, WINO_ACT_SILU = 1, WINO_ACT_GELU = 2,
  *     y[m][n] = act( sum_k x[m][k] * w[n][k] + bias[n] ) + residual[m][n]
  *   x[M][K], residual[M][N], y[M][N]: rows of ldx, ldr, ldy elements (at least as many as they hold), w[N][K] contiguous, bias fp32 [N].
  *   bias and residual may be NULL; residual may be y itself (with ldr = ldy), nothing else may overlap y.
+ *   N is at most 2^26, and every product (backward ones too) has less than 2^24 tiles of 64 x 64.
  */
 size_t wino_linear_workspace_bytes(int M, int N, int K, int dtype, int act);
 int wino_linear(const void *x, const void *w, const float *bias, const void *residual, void *y,
@@ -425,7 +426,9 @@ int wino_glu_backward(const void *x, const void *w, const float *bias, const voi
  *   lse[b][h][i] = log sum_j exp(s_ij), fp32 [B][H][Sq]; NULL where no backward pass follows.
  * Tensors are [batch][position][head][D] with strides of their own in elements (a slice of a packed q,k,v product is read in place);
  * D is contiguous, a multiple of 8, at most 256 (fp32: 160).  Strides are not negative and multiples of 16 bytes; those of outputs
- * are positive and must not let positions overlap.  scale > 0.  Outputs must not overlap inputs.
+ * are positive, and each spans what the smaller ones reach, so that no two positions meet (WINO_ERR_DIM).  scale > 0.  Outputs must
+ * not overlap inputs.  Gradients may share a packed buffer where they have the same strides and none of their positions meet.
+ * H * Sq, B * H * Sq, Skv and B * Hkv * Skv are at most 2^29, B * Hkv at most 2^22.
  */
 typedef struct wino_tensor { void *data; long long stride_b, stride_s, stride_h; } wino_tensor;
 typedef struct wino_attention_args {

@@ -811,27 +811,40 @@ def _scratch(nbytes, like):
     return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
 
 
+def _flat(t):
+    """t as rows of its last dimension, copied where the rows are not contiguous (an expanded gradient, a transposed tensor)."""
+    t = t.reshape(-1, t.shape[-1])
+    ld, step = t.stride()
+    return t if (step == 1 or t.shape[1] == 1) and (ld >= t.shape[1] or t.shape[0] == 1) else t.contiguous()
+
+
+def _packed(t):
+    """t, copied where its channels are not contiguous or a position is not aligned to 16 bytes."""
+    fits = t.stride(-1) == 1 and t.data_ptr() % 16 == 0 and all(s * t.element_size() % 16 == 0 for s in t.stride()[:-1])
+    return t if fits else t.clone(memory_format=torch.contiguous_format)
+
+
 def linear(x, w, bias=None, act: int = WINO_ACT_NONE, residual=None):
     """act(x w^T + bias) + residual over the last dimension of x, with the output and the workspace allocated here."""
-    x2, N = x.reshape(-1, x.shape[-1]), int(w.shape[0])
+    x2, N = _flat(x), int(w.shape[0])
     y = torch.empty((x2.shape[0], N), dtype=x.dtype, device=x.device)
     ws = _scratch(wino_linear_workspace_bytes(x2.shape[0], N, x2.shape[1], DTYPE_OF[x.dtype], act), x)
-    return wino_linear(x2, w, bias, y, act, None if residual is None else residual.reshape(-1, N), ws).view(*x.shape[:-1], N)
+    return wino_linear(x2, w, bias, y, act, None if residual is None else _flat(residual), ws).view(*x.shape[:-1], N)
 
 
 def linear_backward(x, w, bias, dy, act: int = WINO_ACT_NONE):
     """(dx, dw, dbias) of `linear`."""
-    x2, N = x.reshape(-1, x.shape[-1]), int(w.shape[0])
+    x2, N = _flat(x), int(w.shape[0])
     dx, dw = torch.empty(x2.shape, dtype=x.dtype, device=x.device), torch.empty_like(w)
     dbias = torch.empty(N, dtype=torch.float32, device=x.device)
     ws = _scratch(wino_linear_backward_workspace_bytes(x2.shape[0], N, x2.shape[1], DTYPE_OF[x.dtype], act), x)
-    wino_linear_backward(x2, w, bias, dy.reshape(-1, N), dx, dw, dbias, act, ws)
+    wino_linear_backward(x2, w, bias, _flat(dy), dx, dw, dbias, act, ws)
     return dx.view(x.shape), dw, dbias
 
 
 def glu(x, w, bias=None, act: int = WINO_ACT_GELU):
     """(x wu^T + bu) * act(x wg^T + bg) over the last dimension of x."""
-    x2, N = x.reshape(-1, x.shape[-1]), int(w.shape[0]) // 2
+    x2, N = _flat(x), int(w.shape[0]) // 2
     h = torch.empty((x2.shape[0], N), dtype=x.dtype, device=x.device)
     ws = _scratch(wino_glu_workspace_bytes(x2.shape[0], N, x2.shape[1], DTYPE_OF[x.dtype], act), x)
     return wino_glu(x2, w, bias, h, act, ws).view(*x.shape[:-1], N)
@@ -839,16 +852,17 @@ def glu(x, w, bias=None, act: int = WINO_ACT_GELU):
 
 def glu_backward(x, w, bias, dh, act: int = WINO_ACT_GELU):
     """(dx, dw, dbias) of `glu`."""
-    x2, N = x.reshape(-1, x.shape[-1]), int(w.shape[0]) // 2
+    x2, N = _flat(x), int(w.shape[0]) // 2
     dx, dw = torch.empty(x2.shape, dtype=x.dtype, device=x.device), torch.empty_like(w)
     dbias = torch.empty(2 * N, dtype=torch.float32, device=x.device)
     ws = _scratch(wino_glu_backward_workspace_bytes(x2.shape[0], N, x2.shape[1], DTYPE_OF[x.dtype], act), x)
-    wino_glu_backward(x2, w, bias, dh.reshape(-1, N), dx, dw, dbias, act, ws)
+    wino_glu_backward(x2, w, bias, _flat(dh), dx, dw, dbias, act, ws)
     return dx.view(x.shape), dw, dbias
 
 
 def attention(q, k, v, kv_len=None, key_mask=None, scale=None, with_lse: bool = False):
     """softmax(scale q k^T) v; with_lse: (o, lse), what attention_backward takes."""
+    q, k, v = _packed(q), _packed(k), _packed(v)
     (B, Sq, H, D), (_, Skv, Hkv, _) = q.shape, k.shape
     o = torch.empty((B, Sq, H, D), dtype=q.dtype, device=q.device)
     lse = torch.empty((B, H, Sq), dtype=torch.float32, device=q.device) if with_lse else None
@@ -859,6 +873,7 @@ def attention(q, k, v, kv_len=None, key_mask=None, scale=None, with_lse: bool = 
 
 def attention_backward(q, k, v, o, lse, do, kv_len=None, key_mask=None, scale=None):
     """(dq, dk, dv) of `attention`."""
+    q, k, v, o, do = (_packed(t) for t in (q, k, v, o, do))
     (B, Sq, H, D), (_, Skv, Hkv, _) = q.shape, k.shape
     dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
     ws = _scratch(wino_attention_backward_workspace_bytes(B, Sq, Skv, H, Hkv, D, DTYPE_OF[q.dtype]), q)

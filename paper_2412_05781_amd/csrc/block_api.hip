@@ -68,7 +68,7 @@ int run_products(const void* x, long long ldx, const void* w, const void* dz, lo
 }
 
 bool product_dims_ok(int M, int N, int K, int halves) {
-    if (M < 1 || N < 1 || K < 1 || N > (1 << 27)) return false;
+    if (M < 1 || N < 1 || K < 1 || N > (1 << 26)) return false;
     const long long W = (long long)N * halves;
     return gemm_dims_ok(M, W, K) && gemm_dims_ok(M, K, W) && gemm_dims_ok(W, K, M);
 }
@@ -114,8 +114,9 @@ int products_backward(const void* x, const void* w, const float* bias, const voi
 // ---- attention ------------------------------------------------------------------------------------------------------------------------
 bool attention_dims_ok(int B, int Sq, int Skv, int H, int Hkv, int D, int dt) {
     if (B < 1 || Sq < 1 || Skv < 1 || H < 1 || Hkv < 1 || H % Hkv || D < 8 || D % 8 || D > (dt == WINO_F32 ? 160 : 256)) return false;
-    const long long most = 1LL << 30, elements = 1LL << 40;
-    return (long long)H * Sq <= most && Skv <= most && (long long)B * Hkv <= (1LL << 24) && (long long)B * H * Sq <= most && (long long)B * H * Sq * D <= elements &&
+    // (a launch has less than 2^32 threads: 2^24 workgroups of 256, one per 64 or more rows of a head)
+    const long long most = 1LL << 29, elements = 1LL << 40;
+    return (long long)H * Sq <= most && Skv <= most && (long long)B * Hkv <= (1LL << 22) && (long long)B * H * Sq <= most && (long long)B * H * Sq * D <= elements &&
            (long long)B * Hkv * Skv <= most && (long long)B * Hkv * Skv * D <= elements;
 }
 int tensor_status(const wino_tensor& t, size_t es, bool out, int B, int S, int H) {
@@ -132,6 +133,51 @@ int tensor_status(const wino_tensor& t, size_t es, bool out, int B, int S, int H
 size_t tensor_extent(const wino_tensor& t, size_t es, int B, int S, int H, int D) {
     return ((size_t)(B > 1 ? (B - 1) * t.stride_b : 0) + (size_t)(S > 1 ? (S - 1) * t.stride_s : 0) + (size_t)(H > 1 ? (H - 1) * t.stride_h : 0) + (size_t)D) * es;
 }
+
+// A tensor as a lattice of runs of D elements, the widest stride first; dimensions of one position have none.
+struct Lattice { long long stride[3]; int n[3]; int dims; };
+// Of one tensor, or of two that lie among each other: false where they do not have the same strides.
+bool lattices(const wino_tensor& x, const int (&nx)[3], const wino_tensor& y, const int (&ny)[3], Lattice& a, Lattice& b) {
+    const long long sx[3] = {x.stride_b, x.stride_s, x.stride_h}, sy[3] = {y.stride_b, y.stride_s, y.stride_h};
+    a.dims = b.dims = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (nx[i] == 1 && ny[i] == 1) continue;
+        if (nx[i] > 1 && ny[i] > 1 && sx[i] != sy[i]) return false;
+        const long long st = nx[i] > 1 ? sx[i] : sy[i];
+        int at = a.dims++;
+        b.dims = a.dims;
+        for (; at > 0 && a.stride[at - 1] < st; --at) { a.stride[at] = a.stride[at - 1]; a.n[at] = a.n[at - 1]; b.n[at] = b.n[at - 1]; }
+        a.stride[at] = st; a.n[at] = nx[i]; b.n[at] = ny[i];
+    }
+    for (int i = 0; i < 3; ++i) b.stride[i] = a.stride[i];
+    return true;
+}
+// each stride spans what the narrower ones reach
+bool nested(const Lattice& a, int D) {
+    long long reach = D;
+    for (int i = a.dims - 1; i >= 0; --i) {
+        if (a.stride[i] < reach) return false;
+        reach += (a.n[i] - 1) * a.stride[i];
+    }
+    return true;
+}
+// whether a position of a and one of b meet, with b `d` elements behind a; both nested, so that a level's difference is one of the two nearest d
+bool meet(const Lattice& a, const Lattice& b, int level, long long d, int D) {
+    if (level == a.dims) return d > -D && d < D;
+    const long long st = a.stride[level], least = -(long long)(b.n[level] - 1), most = a.n[level] - 1;
+    const long long down = (d >= 0 ? d : d - st + 1) / st;
+    for (long long i = down; i <= down + 1; ++i)
+        if (i >= least && i <= most && meet(a, b, level + 1, d - i * st, D)) return true;
+    return false;
+}
+// Gradients may share a packed buffer: tensors of the same strides whose positions lie between each other's.
+bool gradients_meet(const wino_tensor& x, const int (&nx)[3], const wino_tensor& y, const int (&ny)[3], int D, size_t es) {
+    Lattice a, b;
+    if (!lattices(x, nx, y, ny, a, b) || !nested(a, D) || !nested(b, D)) return true;
+    const long long bytes = (long long)(reinterpret_cast<uintptr_t>(y.data) - reinterpret_cast<uintptr_t>(x.data));
+    return meet(a, b, 0, bytes / (long long)es, D);        // (addresses are multiples of 16)
+}
+
 AttnTensor inner(const wino_tensor& t) { return AttnTensor{t.data, t.stride_b, t.stride_s, t.stride_h}; }
 
 int attention_status(const wino_attention_args* a, bool backward) {
@@ -149,6 +195,14 @@ int attention_status(const wino_attention_args* a, bool backward) {
         const int rc = tensor_status(*items[i].t, es, items[i].out, a->B, items[i].key ? a->Skv : a->Sq, items[i].key ? a->Hkv : a->H);
         if (rc != WINO_OK) return rc;
     }
+    auto count = [&](const Item& x, int (&c)[3]) { c[0] = a->B; c[1] = x.key ? a->Skv : a->Sq; c[2] = x.key ? a->Hkv : a->H; };
+    for (int i = 0; i < n; ++i) {
+        if (!items[i].out) continue;
+        int c[3];
+        Lattice l, same;
+        count(items[i], c);
+        if (!lattices(*items[i].t, c, *items[i].t, c, l, same) || !nested(l, a->D)) return WINO_ERR_DIM;
+    }
     if (backward && !a->lse) return WINO_ERR_NULL;
     if (!at4(a->lse) || !at4(a->kv_len)) return WINO_ERR_ALIGN;
     auto size = [&](const Item& x) { return tensor_extent(*x.t, es, a->B, x.key ? a->Skv : a->Sq, x.key ? a->Hkv : a->H, a->D); };
@@ -158,8 +212,12 @@ int attention_status(const wino_attention_args* a, bool backward) {
         const size_t np = size(items[i]);
         for (int j = 0; j < n; ++j) {
             if (j == i) continue;
-            // gradients may share a packed buffer: only the same place twice is refused there
-            if (items[j].out ? p == items[j].t->data : overlap(p, np, items[j].t->data, size(items[j]))) return WINO_ERR_ALIAS;
+            if (!overlap(p, np, items[j].t->data, size(items[j]))) continue;
+            if (!items[j].out) return WINO_ERR_ALIAS;
+            int ci[3], cj[3];
+            count(items[i], ci);
+            count(items[j], cj);
+            if (gradients_meet(*items[i].t, ci, *items[j].t, cj, a->D, es)) return WINO_ERR_ALIAS;
         }
         if (overlap(p, np, a->lse, (size_t)a->B * a->H * a->Sq * 4) || overlap(p, np, a->kv_len, (size_t)a->B * 4) ||
             overlap(p, np, a->key_mask, (size_t)a->B * a->Skv))

@@ -320,7 +320,7 @@ template <typename E> __global__ void __launch_bounds__(256) column_sums_kernel(
 bool gemm_dims_ok(long long M, long long N, long long K) {
     const long long most = 1LL << 30, elements = 1LL << 40;
     return M >= 1 && N >= 1 && K >= 1 && M <= most && N <= most / 4 && K <= most / 4 && M * N <= elements && M * K <= elements && N * K <= elements &&
-           ((M + kBQ - 1) / kBQ) * ((N + kBP / 2 - 1) / (kBP / 2)) <= (1LL << 26);
+           ((M + kBQ - 1) / kBQ) * ((N + kBP / 2 - 1) / (kBP / 2)) <= (1LL << 24) - 8;      // a launch has less than 2^32 threads: 256 per tile
 }
 
 // one row of sums per 32 rows, per 64 rows twice, per 128 rows twice or four times, or per 256 rows four times

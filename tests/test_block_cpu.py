@@ -165,3 +165,50 @@ def test_binding_refuses_shapes_and_types():
                 lambda: B.wino_attention(q.transpose(2, 3).contiguous().transpose(2, 3), k, k, o), lambda: B.wino_attention(q, k, k, o)):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_outputs_whose_positions_meet_are_refused(L):
+    """Strides that lead two positions of an output to one place, or two gradients of a packed buffer."""
+    fwd = lambda **kw: L.wino_attention(_args(**kw), WS * 2, BIG, None)
+    bwd = lambda **kw: L.wino_attention_backward(_args(**kw), WS * 2, 16, None)         # (accepted calls end at the workspace: nothing is launched)
+    long = dict(B=2, Sq=1, Skv=9000, H=4, Hkv=2, D=64)
+    assert fwd(o=dict(stride_h=8)) == B.WINO_ERR_DIM                                    # heads of 16 channels, 8 apart
+    assert fwd(o=dict(stride_s=32)) == B.WINO_ERR_DIM and fwd(o=dict(stride_b=64)) == B.WINO_ERR_DIM
+    assert fwd(q=dict(stride_h=8), o=dict(stride_h=8)) == B.WINO_ERR_DIM
+    assert L.wino_attention(_args(q=dict(stride_h=8), **long), WS * 2, 16, None) == B.WINO_ERR_WORKSPACE       # inputs may
+    for n in ("dq", "dk", "dv"):
+        assert bwd(**{n: dict(stride_h=8)}) == B.WINO_ERR_DIM, n
+    # one buffer [B][S][dq 4 heads | dk 2 | dv 2][16], Sq = Skv = 5
+    at, row = 0x60000000, 8 * 16
+    place = lambda h, **kw: dict(data=at + h * 32, stride_b=5 * row, stride_s=row, stride_h=16, **kw)
+    ok = dict(Sq=5, dq=place(0), dk=place(4), dv=place(6))
+    assert bwd(**ok) == B.WINO_ERR_WORKSPACE
+    for bad in (dict(dk=place(3)), dict(dv=place(5)), dict(dk=place(6), dv=place(7)), dict(dv=place(7)), dict(dk=place(4 + 8))):
+        assert bwd(**{**ok, **bad}) == (B.WINO_ERR_ALIAS if bad != dict(dk=place(12)) else B.WINO_ERR_WORKSPACE), bad
+    assert bwd(**{**ok, "dv": dict(data=at + 6 * 32, stride_b=5 * row + 8, stride_s=row, stride_h=16)}) == B.WINO_ERR_ALIAS     # other strides
+    # heads outermost: [H][B][S][D] of dq, dk and dv in turn are apart; the same heads are not
+    outer = lambda first, H: dict(data=at + first * 2 * 5 * 16 * 2, stride_b=5 * 16, stride_s=16, stride_h=2 * 5 * 16)
+    assert bwd(Sq=5, dq=outer(0, 4), dk=outer(4, 2), dv=outer(6, 2)) == B.WINO_ERR_WORKSPACE
+    assert bwd(Sq=5, dq=outer(0, 4), dk=outer(3, 2), dv=outer(6, 2)) == B.WINO_ERR_ALIAS
+
+
+def test_sizes_beyond_one_launch_are_refused(L):
+    """A launch has less than 2^32 threads."""
+    assert _linear(L, M=1 << 30, N=1, K=8, ldx=8) == B.WINO_ERR_DIM
+    assert _linear(L, N=1 << 27, K=1) == B.WINO_ERR_DIM
+    assert B.wino_linear_backward_workspace_bytes(8, 1 << 27, 8, B.WINO_F16) == 0
+    assert L.wino_attention(_args(B=1 << 24, Sq=1, Skv=1, H=1, Hkv=1, D=8), None, 0, None) == B.WINO_ERR_DIM
+    assert B.wino_attention_backward_workspace_bytes(1 << 20, 1 << 10, 1, 1, 1, 8, B.WINO_F16) == 0
+
+
+def test_conveniences_take_any_strides():
+    import torch
+    x = torch.zeros(6, 16)
+    assert B._flat(x[:, :8]).data_ptr() == x.data_ptr() and B._flat(x.view(2, 3, 16)).stride() == (16, 1)
+    for t in (x[:1].expand(6, 16), x.t(), x[:, :1].expand(6, 16), x[:1].expand(2, 3, 16)):
+        f = B._flat(t)
+        assert f.stride() == (t.shape[-1], 1) and torch.equal(f, t.reshape(-1, t.shape[-1]))
+    q = torch.zeros(2, 3, 4, 16)
+    assert B._packed(q.transpose(1, 2)).data_ptr() == q.data_ptr()
+    for t in (q.transpose(2, 3), q[:, :, :, :1].expand(2, 3, 4, 16), q.flatten()[2:2 + 2 * 3 * 3 * 16].view(2, 3, 3, 16), torch.zeros(2, 3, 4, 18)[..., :16]):
+        assert B._packed(t).is_contiguous() and B._packed(t).data_ptr() % 16 == 0 and torch.equal(B._packed(t), t)
