@@ -119,6 +119,8 @@ attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int tot
     }
     const unsigned char* kbase = static_cast<const unsigned char*>(a.k.p) + ((long long)b * a.k.b + (long long)hk * a.k.h) * T::ES;
     const unsigned char* vbase = static_cast<const unsigned char*>(a.v.p) + ((long long)b * a.v.b + (long long)hk * a.v.h) * T::ES;
+    KeyMask mask(a, b);
+    if (nsplit == 1) mask.request(0);
     const int len = key_count(a, b), tiles = (len + T::ROWS - 1) / T::ROWS;
     const int t0 = (int)((long long)split * tiles / nsplit), t1 = (int)((long long)(split + 1) * tiles / nsplit);
     using Stream = AttnStream<E, DP>;
@@ -126,7 +128,12 @@ attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int tot
     Stream sk(map, kbase, t0 * T::ROWS, a.k.s), sv(map, vbase, t0 * T::ROWS, a.v.s);
     AttnState<E, DP> st;
     const float c2 = a.scale * kLog2e;
-    auto valid = [&](int t) { return t < t1 ? valid_keys(a, b, t * T::ROWS, len) : 0ull; };
+    if (nsplit > 1) mask.request(t0 * T::ROWS);
+    auto valid = [&](int t) {                              // and the next tile's mask on its way
+        const unsigned long long on = mask.bits(t * T::ROWS, len);
+        mask.request((t + 1) * T::ROWS);
+        return on;
+    };
     auto step = [&](const unsigned char* tk, const unsigned char* tv, unsigned long long on) {
         float16_t s[2] = {};
 #pragma unroll
@@ -224,7 +231,13 @@ attention_few_kernel(AttnArgs a, AttnParts parts, int nsplit) {
     u32x4_t fq[T::KS], lk[F::LOADS], lv[F::LOADS];
     const u32x4_t zero = {0, 0, 0, 0};
     constexpr unsigned long long ALL = F::SUBS == 2 ? ~0ull : 0xffffffffull;
-    auto mask = [&](int t) { return valid_keys(a, b, t * F::KEYS, len) & ALL; };
+    KeyMask keys(a, b);
+    keys.request(t0 * F::KEYS);
+    auto mask = [&](int t) {                               // and the next tile's on its way
+        const unsigned long long on = keys.bits(t * F::KEYS, len) & ALL;
+        keys.request((t + 1) * F::KEYS);
+        return on;
+    };
     auto fetch = [&](int t, unsigned long long on) {
         const unsigned char* kt = kbase + (long long)t * F::KEYS * a.k.s * T::ES;
         const unsigned char* vt = vbase + (long long)t * F::KEYS * a.v.s * T::ES;

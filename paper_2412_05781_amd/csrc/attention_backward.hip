@@ -1,9 +1,9 @@
 // Gradients of attention.  With p = exp(s - lse) from the forward pass and D_i = do_i . o_i:
 //   dv = p^T do,  ds = p (do v^T - D),  dq = scale ds k,  dk = scale ds^T q.
 // Scores are made again, never stored.  Two kernels, both without atomics, so that results do not depend on the order of the workgroups: one owns
-// 64 query rows and streams the keys (dq, and D for the other), one owns 64 keys and streams the query rows of their head (dk, dv; over ranges of
-// the rows, joined in order, where there are few keys).  In either, two waves own 32 rows or keys each and the other two the same ones against the
-// other half of every streamed tile; the halves are added in LDS at the end.
+// query rows and streams the keys (dq, and D for the other), one owns keys and streams the query rows of their head (dk, dv; over ranges of the rows,
+// joined in order, where there are few keys).  In either a wave owns 32 rows or keys: a workgroup 128 (WIDE), or 64 where those would be too few
+// workgroups, with two waves for each 32 that take one half of every streamed tile each; the halves are added in LDS at the end.
 #include "attention_tile.h"
 
 namespace wino {
@@ -17,6 +17,7 @@ struct BackwardParts {
 };
 
 // Two waves a SIMD as long as their registers suffice.
+template <typename E, int DP> constexpr int dq_waves() { return DP <= (sizeof(E) == 2 ? 5 : 4) ? 2 : 1; }
 template <typename E, int DP> constexpr int backward_waves() { return DP <= (sizeof(E) == 2 ? 6 : 4) ? 2 : 1; }
 // Two-byte types keep two tiles in LDS and one on its way; fp32's tiles are too large for that.
 template <typename E> constexpr bool backward_ahead() { return sizeof(E) == 2; }
@@ -40,13 +41,13 @@ template <int N> __device__ __forceinline__ void add_halves(float16_t (&acc)[N],
     }
 }
 
-// 64 query rows: dq, and D_i for the other kernel.
+// Query rows: dq, and D_i for the other kernel.
 //
 // D_i = do_i . o_i from the stored o carries o's rounding, which reaches every ds of the row with the same sign.  But the ds of a row add up to zero, so
 // what they do add up to, r, is that error: D_i + r is right to fp32, and dq less r times the weighted mean of the keys as well.  The mean costs one more
 // product with operands that are there already (4 x 8 x 1024 x 1024 x 80: 35 -> 43 us); the error of dq against 64 bits falls from 1.50 to 1.41 times that of
 // one rounding, which is the rounding of ds and that of dq.
-template <typename E, int DP> __global__ void __launch_bounds__(256, (DP <= (sizeof(E) == 2 ? 5 : 4) ? 2 : 1))
+template <typename E, int DP, bool WIDE> __global__ void __launch_bounds__(256, (dq_waves<E, DP>()))
 attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_xcd) {
     using T = AttnTile<E, DP>;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -54,18 +55,21 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
     if (logical >= total) return;
     const int slot = logical / row_tiles, tile = logical - slot * row_tiles, bh = deal_heads(slot, a.B * a.Hkv), b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
     const AttnRows rows{a.Sq, G * a.Sq};
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, sub = wave >> 1;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, sub = WIDE ? 0 : wave >> 1;
     const typename T::Places places(lane);
-    const int r = tile * 64 + (wave & 1) * 32 + (lane & 31);
+    const int r = tile * (WIDE ? 128 : 64) + (WIDE ? wave : wave & 1) * 32 + (lane & 31);
     const bool row_on = r < rows.R;
     const unsigned char* kbase = static_cast<const unsigned char*>(a.k.p) + ((long long)b * a.k.b + (long long)hk * a.k.h) * T::ES;
     const unsigned char* vbase = static_cast<const unsigned char*>(a.v.p) + ((long long)b * a.v.b + (long long)hk * a.v.h) * T::ES;
+    KeyMask mask(a, b);
+    mask.request(0);
     const int len = key_count(a, b), tiles = (len + T::ROWS - 1) / T::ROWS;
     using Stream = AttnStream<E, DP>;
     const typename Stream::Map map(tid, a.D);
     Stream sk(map, kbase, 0, a.k.s), sv(map, vbase, 0, a.v.s);
     constexpr bool AHEAD = backward_ahead<E>();
-    unsigned long long on = tiles ? valid_keys(a, b, 0, len) : 0;
+    unsigned long long on = mask.bits(0, len);
+    mask.request(T::ROWS);
     if (AHEAD && tiles) {
         sk.fetch(map, on);
         sv.fetch(map, on);
@@ -108,60 +112,65 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
         sk.put(map, tk);
         sv.put(map, tv);
         __syncthreads();
-        const uint32_t cur = (uint32_t)(on >> (32 * sub));
+        const unsigned long long now = on;
         if (t + 1 < tiles) {
-            on = valid_keys(a, b, (t + 1) * T::ROWS, len);
+            on = mask.bits((t + 1) * T::ROWS, len);
+            mask.request((t + 2) * T::ROWS);
             if (AHEAD) {
                 sk.fetch(map, on);
                 sv.fetch(map, on);
             }
         }
-        if (cur == 0) continue;                            // uniform over the wave
-        float16_t s = {}, dp = {};
+#pragma unroll 1
+        for (int h = sub; h < (WIDE ? 2 : sub + 1); ++h) {
+            const uint32_t cur = (uint32_t)(now >> (32 * h));
+            if (cur == 0) continue;                        // uniform over the wave
+            float16_t s = {}, dp = {};
 #pragma unroll
-        for (int ks = 0; ks < T::KS; ++ks) {
-            Mma<E>::run(T::along(tk, 32 * sub, ks, places), fq[ks], s);
-            Mma<E>::run(T::along(tv, 32 * sub, ks, places), fo[ks], dp);
-        }
+            for (int ks = 0; ks < T::KS; ++ks) {
+                Mma<E>::run(T::along(tk, 32 * h, ks, places), fq[ks], s);
+                Mma<E>::run(T::along(tv, 32 * h, ks, places), fo[ks], dp);
+            }
 #pragma unroll
-        for (int q = 0; q < 16; ++q) s[q] = __builtin_amdgcn_exp2f(fmaf(s[q], c2, -lse2));
-        if (cur != 0xffffffffu) {
-            asm volatile("" ::: "memory");                 // a branch
-            const uint32_t mine = cur >> (4 * half);
+            for (int q = 0; q < 16; ++q) s[q] = __builtin_amdgcn_exp2f(fmaf(s[q], c2, -lse2));
+            if (cur != 0xffffffffu) {
+                asm volatile("" ::: "memory");             // a branch
+                const uint32_t mine = cur >> (4 * half);
 #pragma unroll
-            for (int q = 0; q < 16; ++q)
-                if (!((mine >> (8 * (q / 4) + q % 4)) & 1)) s[q] = 0.f;
-        }
+                for (int q = 0; q < 16; ++q)
+                    if (!((mine >> (8 * (q / 4) + q % 4)) & 1)) s[q] = 0.f;
+            }
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
-            dp[q] = s[q] * (dp[q] - dlt);
-            if constexpr (MEAN) rest += dp[q];
-        }
+            for (int q = 0; q < 16; ++q) {
+                dp[q] = s[q] * (dp[q] - dlt);
+                if constexpr (MEAN) rest += dp[q];
+            }
 #pragma unroll
-        for (int st = 0; st < T::ST; ++st) {
-            const u32x4_t w = T::weights(dp, st), wp = MEAN ? T::weights(s, st) : w;
+            for (int st = 0; st < T::ST; ++st) {
+                const u32x4_t w = T::weights(dp, st), wp = MEAN ? T::weights(s, st) : w;
 #pragma unroll
-            for (int d = 0; d < T::NV; ++d) {
-                const u32x4_t keys = T::across(tk, 32 * sub, st, d, places);
-                Mma<E>::run(keys, w, acc[d]);
-                if constexpr (MEAN) Mma<E>::run(keys, wp, acc[T::NV + d]);
+                for (int d = 0; d < T::NV; ++d) {
+                    const u32x4_t keys = T::across(tk, 32 * h, st, d, places);
+                    Mma<E>::run(keys, w, acc[d]);
+                    if constexpr (MEAN) Mma<E>::run(keys, wp, acc[T::NV + d]);
+                }
             }
         }
     }
-    add_halves<NA>(acc, lds, wave, lane);
+    if constexpr (!WIDE) add_halves<NA>(acc, lds, wave, lane);
     if constexpr (MEAN) {
         rest += __shfl_xor(rest, 32);
-        float* t = reinterpret_cast<float*>(lds) + (wave & 1) * 64 + lane;
-        __syncthreads();
-        if (sub) *t = rest;
-        __syncthreads();
-        if (!sub) {
-            rest += *t;
-#pragma unroll
-            for (int d = 0; d < T::NV; ++d)
-#pragma unroll
-                for (int q = 0; q < 16; ++q) acc[d][q] = fmaf(-rest, acc[T::NV + d][q], acc[d][q]);
+        if constexpr (!WIDE) {
+            float* t = reinterpret_cast<float*>(lds) + (wave & 1) * 64 + lane;
+            __syncthreads();
+            if (sub) *t = rest;
+            __syncthreads();
+            if (!sub) rest += *t;
         }
+#pragma unroll
+        for (int d = 0; d < T::NV; ++d)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[d][q] = fmaf(-rest, acc[T::NV + d][q], acc[d][q]);
     }
     if (sub || !row_on) return;
     if (half == 0) delta[row] = dlt + rest;
@@ -175,8 +184,8 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
         }
 }
 
-// 64 keys: dk and dv over one range of the query rows.  Tiles hold rows of one query head each.
-template <typename E, int DP> __global__ void __launch_bounds__(256, (backward_waves<E, DP>()))
+// Keys: dk and dv over one range of the query rows.  Tiles hold rows of one query head each.
+template <typename E, int DP, bool WIDE> __global__ void __launch_bounds__(256, (backward_waves<E, DP>()))
 attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit, int total, int per_xcd) {
     using T = AttnTile<E, DP>;
     constexpr bool AHEAD = backward_ahead<E>();
@@ -187,9 +196,9 @@ attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit,
     const int per_head = key_tiles * nsplit, slot = logical / per_head, in = logical - slot * per_head, split = in / key_tiles, tile = in - split * key_tiles;
     const int bh = deal_heads(slot, a.B * a.Hkv);
     const int b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.H / a.Hkv;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, sub = wave >> 1;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, sub = WIDE ? 0 : wave >> 1;
     const typename T::Places places(lane);
-    const int len = key_count(a, b), key = tile * 64 + (wave & 1) * 32 + (lane & 31);
+    const int len = key_count(a, b), key = tile * (WIDE ? 128 : 64) + (WIDE ? wave : wave & 1) * 32 + (lane & 31);
     const bool in_range = key < a.Skv, key_on = key < len && (!a.key_mask || a.key_mask[(long long)b * a.Skv + key] != 0);
     // acc: dk, then dv.  What a lane whose key is not valid sums stays in its own column and is dropped at the end.
     float16_t acc[2 * T::NV] = {};
@@ -248,34 +257,37 @@ attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit,
             if (tid < T::ROWS) { tl[tid] = nlse; td[tid] = dlt; }
             __syncthreads();
             if (AHEAD && t + 1 < t1) fetch();
-            float16_t s = {}, dp = {};
+#pragma unroll 1
+            for (int h = sub; h < (WIDE ? 2 : sub + 1); ++h) {
+                float16_t s = {}, dp = {};
 #pragma unroll
-            for (int ks = 0; ks < T::KS; ++ks) {
-                Mma<E>::run(T::along(tq, 32 * sub, ks, places), fk[ks], s);
-                Mma<E>::run(T::along(to, 32 * sub, ks, places), fv[ks], dp);
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float4 nl = *reinterpret_cast<const float4*>(tl + 32 * sub + 8 * q + 4 * half), dl = *reinterpret_cast<const float4*>(td + 32 * sub + 8 * q + 4 * half);
-                const float n4[4] = {nl.x, nl.y, nl.z, nl.w}, d4[4] = {dl.x, dl.y, dl.z, dl.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * q + j], c2, n4[j]));
-                    s[4 * q + j] = p;
-                    dp[4 * q + j] = p * (dp[4 * q + j] - d4[j]);
+                for (int ks = 0; ks < T::KS; ++ks) {
+                    Mma<E>::run(T::along(tq, 32 * h, ks, places), fk[ks], s);
+                    Mma<E>::run(T::along(to, 32 * h, ks, places), fv[ks], dp);
                 }
-            }
 #pragma unroll
-            for (int st = 0; st < T::ST; ++st) {
-                const u32x4_t wp = T::weights(s, st), wd = T::weights(dp, st);
+                for (int q = 0; q < 4; ++q) {
+                    const float4 nl = *reinterpret_cast<const float4*>(tl + 32 * h + 8 * q + 4 * half), dl = *reinterpret_cast<const float4*>(td + 32 * h + 8 * q + 4 * half);
+                    const float n4[4] = {nl.x, nl.y, nl.z, nl.w}, d4[4] = {dl.x, dl.y, dl.z, dl.w};
 #pragma unroll
-                for (int d = 0; d < T::NV; ++d) {
-                    Mma<E>::run(T::across(to, 32 * sub, st, d, places), wp, acc[T::NV + d]);
-                    Mma<E>::run(T::across(tq, 32 * sub, st, d, places), wd, acc[d]);
+                    for (int j = 0; j < 4; ++j) {
+                        const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * q + j], c2, n4[j]));
+                        s[4 * q + j] = p;
+                        dp[4 * q + j] = p * (dp[4 * q + j] - d4[j]);
+                    }
+                }
+#pragma unroll
+                for (int st = 0; st < T::ST; ++st) {
+                    const u32x4_t wp = T::weights(s, st), wd = T::weights(dp, st);
+#pragma unroll
+                    for (int d = 0; d < T::NV; ++d) {
+                        Mma<E>::run(T::across(to, 32 * h, st, d, places), wp, acc[T::NV + d]);
+                        Mma<E>::run(T::across(tq, 32 * h, st, d, places), wd, acc[d]);
+                    }
                 }
             }
         }
-        add_halves<2 * T::NV>(acc, lds, wave, lane);
+        if constexpr (!WIDE) add_halves<2 * T::NV>(acc, lds, wave, lane);
     }
     if (sub || !in_range) return;
     if (!key_on) {
@@ -349,6 +361,44 @@ int backward_ranges(int B, int Sq, int Skv, int H, int Hkv, int D, int dt) {
     }
     return best;
 }
+// Whether workgroups own 128 rows, 32 a wave, rather than 64.  Tiles then pass through LDS half as often and no halves are added, but a workgroup has twice
+// the work, which takes it 1.75 times as long (fp32, bound by its MFMAs, 1.95): taken where that beats the rounds in which the chip runs twice as many
+// workgroups of 64.  us with 64 / 128 (B x H x Sq x Skv x D, bf16): 4 x 10 x 1024 x 154 x 64 (dq) 40 / 37, 1 x 10 x 4096 x 4096 x 64 277 / 248,
+// 4 x 16 x 1024 x 1024 x 80 153 / 121, 2 x 8 x 2048 x 2048 x 128 238 / 187; 4 x 8 x 1024 x 1024 x 80 73 / 84.
+bool own_wide(long long heads, int rows, int waves, bool f32) {
+    const long long slots = 256 * waves, narrow = heads * (((long long)rows + 63) / 64), wide = heads * (((long long)rows + 127) / 128);
+    return (double)((narrow + slots - 1) / slots) > (f32 ? 1.95 : 1.75) * (double)((wide + slots - 1) / slots);
+}
+template <typename E, int DP, bool WIDE> hipError_t launch_dq(const AttnArgs& a, float* delta, hipStream_t s) {
+    using T = AttnTile<E, DP>;
+    constexpr int tiles = (backward_ahead<E>() ? 2 : 1) * 2 * T::BYTES, halves = WIDE ? 0 : 2 * 1024 * (T::ES == 2 ? 2 : 1) * T::NV * 4, bytes = tiles > halves ? tiles : halves;
+    static_assert(bytes <= 160 * 1024, "LDS budget");
+    constexpr int own = WIDE ? 128 : 64;
+    const int row_tiles = (a.H / a.Hkv * a.Sq + own - 1) / own;
+    const long long total = (long long)a.B * a.Hkv * row_tiles;
+    if (total > 0xfffff0LL) return hipErrorInvalidValue;
+    auto kern = attention_dq_kernel<E, DP, WIDE>;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (attr != hipSuccess) return attr;
+    const int per_xcd = (int)((total + 7) / 8);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(per_xcd * 8)), dim3(256), bytes, s, a, delta, row_tiles, (int)total, per_xcd);
+    return hipGetLastError();
+}
+template <typename E, int DP, bool WIDE> hipError_t launch_dkv(const AttnArgs& a, const BackwardParts& parts, int nsplit, hipStream_t s) {
+    using T = AttnTile<E, DP>;
+    constexpr int tiles = (backward_ahead<E>() ? 2 : 1) * (2 * T::BYTES + 2 * T::ROWS * 4), halves = WIDE ? 0 : 4 * 1024 * T::NV * 4, bytes = tiles > halves ? tiles : halves;
+    static_assert(bytes <= 160 * 1024, "LDS budget");
+    constexpr int own = WIDE ? 128 : 64;
+    const int key_tiles = (a.Skv + own - 1) / own;
+    const long long total = (long long)a.B * a.Hkv * key_tiles * nsplit;
+    if (total > 0xfffff0LL) return hipErrorInvalidValue;
+    auto kern = attention_dkv_kernel<E, DP, WIDE>;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (attr != hipSuccess) return attr;
+    const int per_xcd = (int)((total + 7) / 8);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(per_xcd * 8)), dim3(256), bytes, s, a, parts, key_tiles, nsplit, (int)total, per_xcd);
+    return hipGetLastError();
+}
 size_t align_floats(size_t n) { return (n + 63) / 64 * 64; }
 
 }  // namespace
@@ -359,11 +409,9 @@ size_t attention_backward_ws_bytes(int B, int Sq, int Skv, int H, int Hkv, int D
 }
 
 hipError_t launch_attention_backward(const AttnArgs& a, int dt, hipStream_t s) {
-    const int R = a.H / a.Hkv * a.Sq, nsplit = backward_ranges(a.B, a.Sq, a.Skv, a.H, a.Hkv, a.D, dt);
-    const int row_tiles = (R + 63) / 64, key_tiles = (a.Skv + 63) / 64;
-    const long long all = (long long)a.B * a.Hkv * R, qt = (long long)a.B * a.Hkv * row_tiles, kt = (long long)a.B * a.Hkv * key_tiles * nsplit;
-    const long long joins = ((long long)a.B * a.Hkv * a.Skv * (a.D / 4) + 255) / 256;
-    if (qt > 0x3fffffffLL || kt > 0x3fffffffLL || joins > 0x7fffffffLL) return hipErrorInvalidValue;
+    const int nsplit = backward_ranges(a.B, a.Sq, a.Skv, a.H, a.Hkv, a.D, dt);
+    const long long all = (long long)a.B * a.H * a.Sq, joins = ((long long)a.B * a.Hkv * a.Skv * (a.D / 4) + 255) / 256;
+    if (nsplit > 1 && joins > 0xffffffLL) return hipErrorInvalidValue;
     BackwardParts parts{a.ws, nullptr, nullptr};
     if (nsplit > 1) {
         parts.dk = a.ws + align_floats((size_t)all);
@@ -375,22 +423,11 @@ hipError_t launch_attention_backward(const AttnArgs& a, int dt, hipStream_t s) {
             constexpr int DP = decltype(dp)::value;
             if constexpr (sizeof(E) == 4 && DP > 10) return hipErrorInvalidValue;
             else {
-                using T = AttnTile<E, DP>;
-                constexpr int buffers = backward_ahead<E>() ? 2 : 1, halves = 2 * 1024 * T::NV * (int)sizeof(float);      // add_halves
-                constexpr int tiles_q = buffers * 2 * T::BYTES, tiles_k = tiles_q + buffers * 2 * T::ROWS * (int)sizeof(float);
-                constexpr int halves_q = T::ES == 2 ? 2 * halves : halves, bytes_q = tiles_q > halves_q ? tiles_q : halves_q, bytes_k = tiles_k > 2 * halves ? tiles_k : 2 * halves;
-                static_assert(bytes_q <= 160 * 1024 && bytes_k <= 160 * 1024, "LDS budget");
-                auto kq = attention_dq_kernel<E, DP>;
-                auto kk = attention_dkv_kernel<E, DP>;
-                static const hipError_t attr_q = hipFuncSetAttribute(reinterpret_cast<const void*>(kq), hipFuncAttributeMaxDynamicSharedMemorySize, bytes_q);
-                static const hipError_t attr_k = hipFuncSetAttribute(reinterpret_cast<const void*>(kk), hipFuncAttributeMaxDynamicSharedMemorySize, bytes_k);
-                if (attr_q != hipSuccess || attr_k != hipSuccess) return hipErrorInvalidValue;
-                const int pq = (int)((qt + 7) / 8), pk = (int)((kt + 7) / 8);
-                hipLaunchKernelGGL(kq, dim3((unsigned)(pq * 8)), dim3(256), bytes_q, s, a, parts.delta, row_tiles, (int)qt, pq);
-                hipError_t e = hipGetLastError();
+                const bool wide_q = own_wide((long long)a.B * a.Hkv, a.H / a.Hkv * a.Sq, dq_waves<E, DP>(), sizeof(E) == 4);
+                const bool wide_k = own_wide((long long)a.B * a.Hkv * nsplit, a.Skv, backward_waves<E, DP>(), sizeof(E) == 4);
+                const hipError_t e = wide_q ? launch_dq<E, DP, true>(a, parts.delta, s) : launch_dq<E, DP, false>(a, parts.delta, s);
                 if (e != hipSuccess) return e;
-                hipLaunchKernelGGL(kk, dim3((unsigned)(pk * 8)), dim3(256), bytes_k, s, a, parts, key_tiles, nsplit, (int)kt, pk);
-                return hipGetLastError();
+                return wide_k ? launch_dkv<E, DP, true>(a, parts, nsplit, s) : launch_dkv<E, DP, false>(a, parts, nsplit, s);
             }
         });
         if (rc != hipSuccess || nsplit == 1) return rc;

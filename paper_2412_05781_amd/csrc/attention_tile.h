@@ -163,13 +163,20 @@ template <typename E> __device__ __forceinline__ void store_channels(unsigned ch
     else *reinterpret_cast<uint2*>(row + c * 2) = make_uint2(pack_pair<E>(v[0], v[1]), pack_pair<E>(v[2], v[3]));
 }
 
-// Valid keys among the 64 from key0 on, one bit each: below the row's length and not masked.  Called by whole waves.
-__device__ __forceinline__ unsigned long long valid_keys(const AttnArgs& a, int b, int key0, int len) {
-    const int key = key0 + (int)(threadIdx.x & 63);
-    bool ok = key < len;
-    if (a.key_mask && ok) ok = a.key_mask[(long long)b * a.Skv + key] != 0;
-    return __ballot(ok);
-}
+// Valid keys among 64, one bit each: below the row's length and not masked.  A tile's mask is requested a tile before its bits are asked for, so that
+// the loads of keys and values do not wait for it (and the first one not for the length).  Called by whole waves.
+struct KeyMask {
+    const unsigned char* mask;       // null: every key
+    int Skv;
+    uint32_t raw = 1;
+    __device__ __forceinline__ KeyMask(const AttnArgs& a, int b) : mask(a.key_mask ? a.key_mask + (long long)b * a.Skv : nullptr), Skv(a.Skv) {}
+    __device__ __forceinline__ void request(int key0) {
+        const int key = key0 + (int)(threadIdx.x & 63);
+        if (mask) raw = key < Skv ? mask[key] : 0;
+    }
+    // of the tile requested last
+    __device__ __forceinline__ unsigned long long bits(int key0, int len) const { return __ballot(key0 + (int)(threadIdx.x & 63) < len && raw); }
+};
 __device__ __forceinline__ int key_count(const AttnArgs& a, int b) {
     if (!a.kv_len) return a.Skv;
     const int n = a.kv_len[b];

@@ -421,3 +421,13 @@ def test_long_sizes_against_float32_products():
         assert ((db - dz.sum(0)).norm() / db.norm()).item() <= 1e-5
         y = B.linear(got, w[:K, :].T.contiguous().view(K, K).repeat(1, 4).contiguous(), None, residual=x)
         assert torch.isfinite(y).all()
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D", [(t, H, Hkv, D) for t in TYPES
+                                           for H, Hkv, D in [(64, 64, 40), (64, 64, 64), (64, 64, 72), (40, 40, 128), (40, 20, 128), (40, 40, 152), (40, 40, 200)]
+                                           if t != F32 or D <= 160])
+def test_attention_of_many_heads(dtype, H, Hkv, D):
+    """Enough rows and keys that the backward pass's workgroups own 128 of them."""
+    mask = torch.rand((2, 258), generator=torch.Generator().manual_seed(D)) < 0.9
+    mask[1, 64:130] = False
+    _check_attention(2, 260, 258, H, Hkv, D, dtype, lens=[258, 200], mask=mask)
