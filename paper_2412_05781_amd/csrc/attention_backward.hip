@@ -19,8 +19,9 @@ struct BackwardParts {
 // Two waves a SIMD as long as their registers suffice.
 template <typename E, int DP> constexpr int dq_waves() { return DP <= (sizeof(E) == 2 ? 5 : 4) ? 2 : 1; }
 template <typename E, int DP> constexpr int backward_waves() { return DP <= (sizeof(E) == 2 ? 6 : 4) ? 2 : 1; }
-// Two-byte types keep two tiles in LDS and one on its way; fp32's tiles are too large for that.
-template <typename E> constexpr bool backward_ahead() { return sizeof(E) == 2; }
+// Two-byte types keep two tiles in LDS and one on its way, except where its registers and addresses cost more than it hides: us with / without, for
+// 2 x 8 x 1024 x 1024 x D (128: 2 x 8 x 2048 x 2048): D 96 57 / 58, 128 187 / 173, 160 94 / 99, 256 366 / 153 (registers spill).  fp32's tiles are too large for it.
+template <typename E, int DP> constexpr bool backward_ahead() { return sizeof(E) == 2 && (DP <= 6 || DP == 10); }
 
 // adds the accumulators of waves 2 and 3 to those of waves 0 and 1, through LDS; called by the whole workgroup
 template <int N> __device__ __forceinline__ void add_halves(float16_t (&acc)[N], unsigned char* lds, int wave, int lane) {
@@ -67,7 +68,7 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
     using Stream = AttnStream<E, DP>;
     const typename Stream::Map map(tid, a.D);
     Stream sk(map, kbase, 0, a.k.s), sv(map, vbase, 0, a.v.s);
-    constexpr bool AHEAD = backward_ahead<E>();
+    constexpr bool AHEAD = backward_ahead<E, DP>();
     unsigned long long on = mask.bits(0, len);
     mask.request(T::ROWS);
     if (AHEAD && tiles) {
@@ -188,7 +189,7 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
 template <typename E, int DP, bool WIDE> __global__ void __launch_bounds__(256, (backward_waves<E, DP>()))
 attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit, int total, int per_xcd) {
     using T = AttnTile<E, DP>;
-    constexpr bool AHEAD = backward_ahead<E>();
+    constexpr bool AHEAD = backward_ahead<E, DP>();
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     float* stats = reinterpret_cast<float*>(lds + (AHEAD ? 4 : 2) * T::BYTES);        // per buffer: -lse (base 2) and D of the tile's rows
     const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
@@ -371,7 +372,7 @@ bool own_wide(long long heads, int rows, int waves, bool f32) {
 }
 template <typename E, int DP, bool WIDE> hipError_t launch_dq(const AttnArgs& a, float* delta, hipStream_t s) {
     using T = AttnTile<E, DP>;
-    constexpr int tiles = (backward_ahead<E>() ? 2 : 1) * 2 * T::BYTES, halves = WIDE ? 0 : 2 * 1024 * (T::ES == 2 ? 2 : 1) * T::NV * 4, bytes = tiles > halves ? tiles : halves;
+    constexpr int tiles = (backward_ahead<E, DP>() ? 2 : 1) * 2 * T::BYTES, halves = WIDE ? 0 : 2 * 1024 * (T::ES == 2 ? 2 : 1) * T::NV * 4, bytes = tiles > halves ? tiles : halves;
     static_assert(bytes <= 160 * 1024, "LDS budget");
     constexpr int own = WIDE ? 128 : 64;
     const int row_tiles = (a.H / a.Hkv * a.Sq + own - 1) / own;
@@ -386,7 +387,7 @@ template <typename E, int DP, bool WIDE> hipError_t launch_dq(const AttnArgs& a,
 }
 template <typename E, int DP, bool WIDE> hipError_t launch_dkv(const AttnArgs& a, const BackwardParts& parts, int nsplit, hipStream_t s) {
     using T = AttnTile<E, DP>;
-    constexpr int tiles = (backward_ahead<E>() ? 2 : 1) * (2 * T::BYTES + 2 * T::ROWS * 4), halves = WIDE ? 0 : 4 * 1024 * T::NV * 4, bytes = tiles > halves ? tiles : halves;
+    constexpr int tiles = (backward_ahead<E, DP>() ? 2 : 1) * (2 * T::BYTES + 2 * T::ROWS * 4), halves = WIDE ? 0 : 4 * 1024 * T::NV * 4, bytes = tiles > halves ? tiles : halves;
     static_assert(bytes <= 160 * 1024, "LDS budget");
     constexpr int own = WIDE ? 128 : 64;
     const int key_tiles = (a.Skv + own - 1) / own;
