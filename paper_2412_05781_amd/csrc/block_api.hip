@@ -50,18 +50,21 @@ BackwardSpace backward_space(int M, int W, int K, int dt, bool stored) {
     return b;
 }
 
-// dx = dz w and dw = dz^T x, in one launch where both are asked for
-int run_products(const void* x, long long ldx, const void* w, const void* dz, long long lddz, void* dx, long long lddx, void* dw, int M, int W, int K, void* scratch, int dt, hipStream_t s) {
+// dx = dz w and dw = dz^T x, in one launch where both are asked for; and the column sums of dz
+int run_products(const void* x, long long ldx, const void* w, const void* dz, long long lddz, void* dx, long long lddx, void* dw, const ColumnSums& c, int M, int W, int K,
+                 void* scratch, int dt, hipStream_t s) {
     Product a{Operand{w, K}, Operand{dz, lddz}, GemmShape{M, K, W}, Epilogue(), gemm_ranges(M, K, W, dt)};
     Product b{Operand{x, ldx}, Operand{dz, lddz}, GemmShape{W, K, M}, Epilogue(), gemm_ranges(W, K, M, dt)};
     a.e.out = dx; a.e.ld_out = lddx;
     b.e.out = dw; b.e.ld_out = K;
+    if ((!dx || !dw) && c.out && launch_column_sums(c, dt, s) != hipSuccess) return WINO_ERR_HIP;
+    if (!dx && !dw) return WINO_OK;
     if (!dw) return product(EP_STORE, true, false, a.P, a.Q, a.g, a.e, scratch, dt, s) == hipSuccess ? WINO_OK : WINO_ERR_HIP;
     if (!dx) return product(EP_STORE, true, true, b.P, b.Q, b.g, b.e, scratch, dt, s) == hipSuccess ? WINO_OK : WINO_ERR_HIP;
     unsigned char* base = static_cast<unsigned char*>(scratch);
     if (a.nsplit > 1) a.e.part = reinterpret_cast<float*>(base);
     if (b.nsplit > 1) b.e.part = reinterpret_cast<float*>(base + product_bytes(M, K, W, dt));
-    if (launch_gemm_pair(a, b, dt, s) != hipSuccess) return WINO_ERR_HIP;
+    if (launch_gemm_pair(a, b, c, dt, s) != hipSuccess) return WINO_ERR_HIP;
     for (const Product* p : {&a, &b})
         if (p->nsplit > 1 && launch_join(p->e.part, p->nsplit, p->g, p->e, dt, s) != hipSuccess) return WINO_ERR_HIP;
     return WINO_OK;
@@ -98,17 +101,18 @@ int products_backward(const void* x, const void* w, const float* bias, const voi
     float* sums = reinterpret_cast<float*>(base + b.dz);
     const void* dz = dy;
     long long lddz = lddy;
+    ColumnSums c{dy, lddy, M, N, nullptr};
     if (stored) {
         Epilogue e;
         e.bias = bias; e.extra = dy; e.ld_extra = lddy; e.out = base; e.ld_out = b.ld; e.sums = sums; e.act = act;
         if (launch_gemm(halves == 2 ? EP_DGLU : EP_DLINEAR, false, false, Operand{w, K}, Operand{x, ldx}, GemmShape{M, N, K}, e, 1, dt, s, &b.sum_rows) != hipSuccess) return WINO_ERR_HIP;
         dz = base; lddz = b.ld;
-    } else if (dbias && launch_column_sums(dy, lddy, M, N, b.sum_rows == 1 ? dbias : sums, dt, s) != hipSuccess) {
-        return WINO_ERR_HIP;
+    } else if (dbias) {
+        c.out = b.sum_rows == 1 ? dbias : sums;
     }
-    if (dbias && (stored || b.sum_rows > 1) && launch_sum_rows(sums, b.sum_rows, W, dbias, s) != hipSuccess) return WINO_ERR_HIP;
-    if (!dx && !dw) return WINO_OK;
-    return run_products(x, ldx, w, dz, lddz, dx, lddx, dw, M, W, K, base + b.dz + b.sums, dt, s);
+    const int rc = run_products(x, ldx, w, dz, lddz, dx, lddx, dw, c, M, W, K, base + b.dz + b.sums, dt, s);
+    if (rc != WINO_OK || !dbias || c.out == dbias) return rc;
+    return launch_sum_rows(sums, b.sum_rows, W, dbias, s) == hipSuccess ? WINO_OK : WINO_ERR_HIP;
 }
 
 // ---- attention ------------------------------------------------------------------------------------------------------------------------

@@ -49,17 +49,19 @@ int gemm_most_sum_rows(int M);
 int gemm_ranges(int M, int N, int K, int dt);
 hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit,
                        int dt, hipStream_t s, int* sum_rows = nullptr);
-// a = dz w (P across, Q along the reduction) and b = dz^T x (both across), with EP_STORE or ranges
-hipError_t launch_gemm_pair(const Product& a, const Product& b, int dt, hipStream_t s);
+// Sums over the rows of x[M][N], in column_sum_rows(M) ranges: out[range][n].  out null: not asked for.
+struct ColumnSums { const void* x; long long ld; int M, N; float* out; };
+// a = dz w (P across, Q along the reduction) and b = dz^T x (both across), with EP_STORE or ranges; and the column sums c
+hipError_t launch_gemm_pair(const Product& a, const Product& b, const ColumnSums& c, int dt, hipStream_t s);
 // x W^T with EP_LINEAR or (glu) EP_GLU for few rows, one kernel, no workspace
 bool few_gemm_ok(int M);
 hipError_t launch_few_gemm(bool glu, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s);
 // out = act(sum over ranges + bias) + extra
 hipError_t launch_join(const float* part, int nsplit, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s);
-// column sums: out[c] = sum over rows of part[row][c]; and of a stored tensor, in two steps
+// out[c] = sum over rows of part[row][c]
 hipError_t launch_sum_rows(const float* part, int rows, int cols, float* out, hipStream_t s);
-int column_sum_rows(int M);          // 1: launch_column_sums writes the sums themselves
-hipError_t launch_column_sums(const void* x, long long ld, int M, int N, float* part, int dt, hipStream_t s);
+int column_sum_rows(int M);
+hipError_t launch_column_sums(const ColumnSums& c, int dt, hipStream_t s);
 
 // One call of the attention operators; strides in elements, the last dimension contiguous.
 struct AttnTensor { const void* p; long long b, s, h; };

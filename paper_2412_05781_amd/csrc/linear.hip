@@ -279,40 +279,9 @@ __global__ void __launch_bounds__(1024) sum_rows_kernel(const float* part, int r
     }
 }
 
-// 64 columns x a range of rows per workgroup; eight lanes a row, eight rows a wave at a time
-template <typename E> __global__ void __launch_bounds__(256) column_sums_kernel(const E* x, long long ld, int M, int N, float* part, bool vec) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c0 = blockIdx.x * 64 + (lane & 7) * 8, left = N - c0;
-    const long long r0 = (long long)blockIdx.y * M / gridDim.y, r1 = (long long)(blockIdx.y + 1) * M / gridDim.y;
-    __shared__ float t[4][64];
-    float a[8] = {};
-    if (vec && left >= 8) {
-#pragma unroll 4
-        for (long long r = r0 + w * 8 + (lane >> 3); r < r1; r += 32) {
-            const E* p = x + r * ld + c0;
-            if constexpr (sizeof(E) == 4) {
-                const float4 u = reinterpret_cast<const float4*>(p)[0], v = reinterpret_cast<const float4*>(p)[1];
-                a[0] += u.x; a[1] += u.y; a[2] += u.z; a[3] += u.w; a[4] += v.x; a[5] += v.y; a[6] += v.z; a[7] += v.w;
-            } else {
-                const uint4 u = *reinterpret_cast<const uint4*>(p);
-                a[0] += lo16<E>(u.x); a[1] += hi16<E>(u.x); a[2] += lo16<E>(u.y); a[3] += hi16<E>(u.y);
-                a[4] += lo16<E>(u.z); a[5] += hi16<E>(u.z); a[6] += lo16<E>(u.w); a[7] += hi16<E>(u.w);
-            }
-        }
-    } else {
-        for (long long r = r0 + w * 8 + (lane >> 3); r < r1; r += 32)
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < left) a[i] += to_f32<E>(x[r * ld + c0 + i]);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-#pragma unroll
-        for (int d = 8; d < 64; d <<= 1) a[i] += __shfl_xor(a[i], d);
-        if (lane < 8) t[w][lane * 8 + i] = a[i];
-    }
-    __syncthreads();
-    const int c = blockIdx.x * 64 + threadIdx.x;
-    if (threadIdx.x < 64 && c < N) part[(size_t)blockIdx.y * N + c] = (t[0][threadIdx.x] + t[1][threadIdx.x]) + (t[2][threadIdx.x] + t[3][threadIdx.x]);
+template <typename E> __global__ void __launch_bounds__(256) column_sums_kernel(ColumnSums c, bool vec) {
+    __shared__ float t[4 * 64];
+    column_sums<E, 4>(c, vec, blockIdx.x, blockIdx.y, gridDim.y, t);
 }
 
 }  // namespace
@@ -365,10 +334,11 @@ hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, con
     });
 }
 
-hipError_t launch_gemm_pair(const Product& a, const Product& b, int dt, hipStream_t s) {
+hipError_t launch_gemm_pair(const Product& a, const Product& b, const ColumnSums& c, int dt, hipStream_t s) {
     const int ea = a.e.part ? EP_PART : EP_STORE, eb = b.e.part ? EP_PART : EP_STORE;
-    if (tile_gemm_ok(ea, true, false, a.P, a.Q, a.g, a.e, dt) && tile_gemm_ok(eb, true, true, b.P, b.Q, b.g, b.e, dt)) return launch_tile_pair(a, b, dt, s);
-    const hipError_t rc = launch_gemm(ea, true, false, a.P, a.Q, a.g, a.e, a.nsplit, dt, s);
+    if (tile_gemm_ok(ea, true, false, a.P, a.Q, a.g, a.e, dt) && tile_gemm_ok(eb, true, true, b.P, b.Q, b.g, b.e, dt)) return launch_tile_pair(a, b, c, dt, s);
+    hipError_t rc = c.out ? launch_column_sums(c, dt, s) : hipSuccess;
+    if (rc == hipSuccess) rc = launch_gemm(ea, true, false, a.P, a.Q, a.g, a.e, a.nsplit, dt, s);
     return rc != hipSuccess ? rc : launch_gemm(eb, true, true, b.P, b.Q, b.g, b.e, b.nsplit, dt, s);
 }
 
@@ -396,11 +366,10 @@ hipError_t launch_sum_rows(const float* part, int rows, int cols, float* out, hi
 
 int column_sum_rows(int M) { return M <= 1024 ? 1 : M < 256 * 64 ? M / 256 : 64; }
 
-hipError_t launch_column_sums(const void* x, long long ld, int M, int N, float* part, int dt, hipStream_t s) {
+hipError_t launch_column_sums(const ColumnSums& c, int dt, hipStream_t s) {
     return with_dtype(dt, [&](auto* tag) -> hipError_t {
         using E = std::remove_pointer_t<decltype(tag)>;
-        hipLaunchKernelGGL((column_sums_kernel<E>), dim3((unsigned)((N + 63) / 64), (unsigned)column_sum_rows(M)), dim3(256), 0, s, (const E*)x, ld, M, N, part,
-                           ((reinterpret_cast<uintptr_t>(x) | (uintptr_t)(ld * (long long)sizeof(E))) & 15u) == 0);
+        hipLaunchKernelGGL((column_sums_kernel<E>), dim3((unsigned)((c.N + 63) / 64), (unsigned)column_sum_rows(c.M)), dim3(256), 0, s, c, vec_rows<E>(Operand{c.x, c.ld}));
         return hipGetLastError();
     });
 }

@@ -104,7 +104,48 @@ template <typename E> inline bool vec_rows(const Operand& o) {
 bool tile_gemm_ok(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int dt);
 hipError_t launch_tile_gemm(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, int dt, hipStream_t s, int* sum_rows);
 
-// two products in one launch: a with P across and Q along the reduction, b with both across
-hipError_t launch_tile_pair(const Product& a, const Product& b, int dt, hipStream_t s);
+// two products in one launch: a with P across and Q along the reduction, b with both across; and the column sums, where c.out is set
+hipError_t launch_tile_pair(const Product& a, const Product& b, const ColumnSums& c, int dt, hipStream_t s);
+
+// Column sums of 64 columns x one of `ranges` ranges of rows by a workgroup of NW waves; eight lanes a row, eight rows a wave at a time.  t: 64 NW floats in LDS.
+template <typename E, int NW> __device__ __forceinline__ void column_sums(const ColumnSums& c, bool vec, int block, int range, int ranges, float* t) {
+    const E* x = static_cast<const E*>(c.x);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c0 = block * 64 + (lane & 7) * 8, left = c.N - c0;
+    const long long r0 = (long long)range * c.M / ranges, r1 = (long long)(range + 1) * c.M / ranges;
+    float a[8] = {};
+    if (vec && left >= 8) {
+#pragma unroll 4
+        for (long long r = r0 + w * 8 + (lane >> 3); r < r1; r += 8 * NW) {
+            const E* p = x + r * c.ld + c0;
+            if constexpr (sizeof(E) == 4) {
+                const float4 u = reinterpret_cast<const float4*>(p)[0], v = reinterpret_cast<const float4*>(p)[1];
+                a[0] += u.x; a[1] += u.y; a[2] += u.z; a[3] += u.w; a[4] += v.x; a[5] += v.y; a[6] += v.z; a[7] += v.w;
+            } else {
+                const uint4 u = *reinterpret_cast<const uint4*>(p);
+                a[0] += lo16<E>(u.x); a[1] += hi16<E>(u.x); a[2] += lo16<E>(u.y); a[3] += hi16<E>(u.y);
+                a[4] += lo16<E>(u.z); a[5] += hi16<E>(u.z); a[6] += lo16<E>(u.w); a[7] += hi16<E>(u.w);
+            }
+        }
+    } else {
+        for (long long r = r0 + w * 8 + (lane >> 3); r < r1; r += 8 * NW)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) a[i] += to_f32<E>(x[r * c.ld + c0 + i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int d = 8; d < 64; d <<= 1) a[i] += __shfl_xor(a[i], d);
+        if (lane < 8) t[w * 64 + lane * 8 + i] = a[i];
+    }
+    __syncthreads();
+    const int col = block * 64 + threadIdx.x;
+    if (threadIdx.x < 64 && col < c.N) {
+        float v = 0.f;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) v += t[i * 64 + threadIdx.x];
+        c.out[(size_t)range * c.N + col] = v;
+    }
+}
 
 }  // namespace wino
