@@ -101,12 +101,13 @@ int products_backward(const void* x, const void* w, const float* bias, const voi
     float* sums = reinterpret_cast<float*>(base + b.dz);
     const void* dz = dy;
     long long lddz = lddy;
-    ColumnSums c{dy, lddy, M, N, nullptr};
+    ColumnSums c{dy, lddy, M, N, nullptr, b.sum_rows, false};
     if (stored) {
         Epilogue e;
         e.bias = bias; e.extra = dy; e.ld_extra = lddy; e.out = base; e.ld_out = b.ld; e.sums = sums; e.act = act;
         if (launch_gemm(halves == 2 ? EP_DGLU : EP_DLINEAR, false, false, Operand{w, K}, Operand{x, ldx}, GemmShape{M, N, K}, e, 1, dt, s, &b.sum_rows) != hipSuccess) return WINO_ERR_HIP;
         dz = base; lddz = b.ld;
+        if (dbias) c = ColumnSums{sums, W, b.sum_rows, W, dbias, 1, true};
     } else if (dbias) {
         c.out = b.sum_rows == 1 ? dbias : sums;
     }

@@ -49,8 +49,8 @@ int gemm_most_sum_rows(int M);
 int gemm_ranges(int M, int N, int K, int dt);
 hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit,
                        int dt, hipStream_t s, int* sum_rows = nullptr);
-// Sums over the rows of x[M][N], in column_sum_rows(M) ranges: out[range][n].  out null: not asked for.
-struct ColumnSums { const void* x; long long ld; int M, N; float* out; };
+// Sums over the rows of x[M][N], in `ranges` ranges: out[range][n].  out null: not asked for.  f32: x is fp32 whatever the call's type, in one range.
+struct ColumnSums { const void* x; long long ld; int M, N; float* out; int ranges; bool f32; };
 // a = dz w (P across, Q along the reduction) and b = dz^T x (both across), with EP_STORE or ranges; and the column sums c
 hipError_t launch_gemm_pair(const Product& a, const Product& b, const ColumnSums& c, int dt, hipStream_t s);
 // x W^T with EP_LINEAR or (glu) EP_GLU for few rows, one kernel, no workspace

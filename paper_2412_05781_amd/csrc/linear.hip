@@ -367,9 +367,10 @@ hipError_t launch_sum_rows(const float* part, int rows, int cols, float* out, hi
 int column_sum_rows(int M) { return M <= 1024 ? 1 : M < 256 * 64 ? M / 256 : 64; }
 
 hipError_t launch_column_sums(const ColumnSums& c, int dt, hipStream_t s) {
+    if (c.f32) return launch_sum_rows(static_cast<const float*>(c.x), c.M, c.N, c.out, s);
     return with_dtype(dt, [&](auto* tag) -> hipError_t {
         using E = std::remove_pointer_t<decltype(tag)>;
-        hipLaunchKernelGGL((column_sums_kernel<E>), dim3((unsigned)((c.N + 63) / 64), (unsigned)column_sum_rows(c.M)), dim3(256), 0, s, c, vec_rows<E>(Operand{c.x, c.ld}));
+        hipLaunchKernelGGL((column_sums_kernel<E>), dim3((unsigned)((c.N + 63) / 64), (unsigned)c.ranges), dim3(256), 0, s, c, vec_rows<E>(Operand{c.x, c.ld}));
         return hipGetLastError();
     });
 }

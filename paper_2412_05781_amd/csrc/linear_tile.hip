@@ -435,16 +435,18 @@ __global__ void __launch_bounds__(WP * WQ * 64) gemm_tile_kernel(Operand P, Oper
 }
 
 // Two products in one launch, dz w (P across, Q along) and dz^T x (both across): either alone has few tiles and long reductions, together they fill the
-// chip.  XCD by XCD the first one's tiles, then the second one's.  Column sums of dz, where they are asked for, are made by workgroups of their own in
-// front of them (616 x 2048 x 1280: 5.6 us as a launch before).
+// chip.  XCD by XCD the first one's tiles, then the second one's.  The bias gradient, where it is asked for, is summed by workgroups of its own in
+// front of them (616 x 2048 x 1280: 5.6 us as a launch before; 4096 x 640 x 2 x 2560: 5.1 us after).
 struct PairPart { Operand P, Q; GemmShape g; Epilogue e; int tiles_p, tiles_q, total, per_xcd, nsplit; };
 template <typename E, int BP, int BQ, int WP, int WQ, int NST>
-__global__ void __launch_bounds__(WP * WQ * 64) gemm_pair_kernel(PairPart a, PairPart b, ColumnSums c, int sum_blocks, int sum_ranges, int sum_per_xcd) {
+__global__ void __launch_bounds__(WP * WQ * 64) gemm_pair_kernel(PairPart a, PairPart b, ColumnSums c, bool vec, int sum_blocks, int sum_per_xcd) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int xcd = blockIdx.x % 8, at = (int)(blockIdx.x / 8) - sum_per_xcd;
     if (at < 0) {
         const int id = blockIdx.x, range = id / sum_blocks;
-        if (range < sum_ranges) column_sums<E, WP * WQ>(c, true, id - range * sum_blocks, range, sum_ranges, reinterpret_cast<float*>(lds));
+        if (range >= c.ranges) return;
+        if (c.f32) column_sums<float, WP * WQ>(c, vec, id - range * sum_blocks, range, c.ranges, reinterpret_cast<float*>(lds));
+        else column_sums<E, WP * WQ>(c, vec, id - range * sum_blocks, range, c.ranges, reinterpret_cast<float*>(lds));
     } else if (at < a.per_xcd) {
         const int logical = xcd * a.per_xcd + at;
         if (logical < a.total) gemm_tile<E, EP_STORE, true, false, BP, BQ, WP, WQ, NST>(a.P, a.Q, a.g, a.e, a.tiles_p, a.tiles_q, a.nsplit, logical, lds);
@@ -524,8 +526,10 @@ template <typename E, int BP, int BQ, int WP, int WQ, int NST> hipError_t launch
     auto kern = gemm_pair_kernel<E, BP, BQ, WP, WQ, NST>;
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (attr != hipSuccess) return attr;
-    const int sum_blocks = c.out ? (c.N + 63) / 64 : 0, sum_ranges = c.out ? column_sum_rows(c.M) : 0, sum_per_xcd = (sum_blocks * sum_ranges + 7) / 8;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((sum_per_xcd + a.per_xcd + b.per_xcd) * 8)), dim3(WP * WQ * 64), bytes, s, a, b, c, sum_blocks, sum_ranges, sum_per_xcd);
+    const int sum_blocks = c.out ? (c.N + 63) / 64 : 0, sum_per_xcd = (sum_blocks * c.ranges + 7) / 8;
+    const Operand x{c.x, c.ld};
+    const bool vec = c.f32 ? vec_rows<float>(x) : vec_rows<E>(x);
+    hipLaunchKernelGGL(kern, dim3((unsigned)((sum_per_xcd + a.per_xcd + b.per_xcd) * 8)), dim3(WP * WQ * 64), bytes, s, a, b, c, vec, sum_blocks, sum_per_xcd);
     return hipGetLastError();
 }
 
