@@ -7,16 +7,19 @@ namespace wino {
 // Normal distribution function P(z) = (1 + erf(z / sqrt 2)) / 2 and density p(z).  Two-byte storage: erf by formula 7.1.26 of Abramowitz and Stegun,
 // Handbook of Mathematical Functions (absolute error 1.5e-7, a 2600th of fp16's half step at 1), whose exponential is the density's as well: one
 // exponential and one reciprocal for both.  fp32 storage: the library's erff.
+__device__ __forceinline__ float normal_tail(float z, float& ex) {                       // P(-|z|), and exp(-z^2 / 2)
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+    ex = __builtin_amdgcn_exp2f(-0.72134752f * z * z);
+    const float poly = fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f), 0.5f * -0.284496736f), 0.5f * 0.254829592f);
+    return t * poly * ex;
+}
 template <typename E> __device__ __forceinline__ void normal_cdf(float z, float& cdf, float& pdf) {
     if constexpr (sizeof(E) == 4) {
         cdf = 0.5f * (1.f + erff(z * 0.70710678f));
         pdf = 0.39894228f * expf(-0.5f * z * z);
     } else {
-        const float a = fabsf(z) * 0.70710678f;
-        const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.f));
-        const float ex = __builtin_amdgcn_exp2f(-0.72134752f * z * z);              // exp(-z^2 / 2)
-        const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-        const float tail = 0.5f * poly * ex;                                       // P(-|z|)
+        float ex;
+        const float tail = normal_tail(z, ex);
         cdf = z < 0.f ? tail : 1.f - tail;
         pdf = 0.39894228f * ex;
     }
@@ -29,9 +32,10 @@ template <typename E> __device__ __forceinline__ float logistic(float z) {
 }
 
 // Every activation here is z * c(z) with a distribution function c; its derivative is c + z c'.  An infinite z gives 0 at one end and z at
-// the other, as the limit says, where the product would be NaN.
+// the other, as the limit says, where the product would be NaN: c and c' have reached their limits long before 1000.
 template <typename E, int ACT> __device__ __forceinline__ void act_both(float z, float& a, float& slope) {
     if constexpr (ACT == ACT_NONE) { a = z; slope = 1.f; return; }
+    const float zc = __builtin_amdgcn_fmed3f(z, -1000.f, 1000.f);
     float c, d;
     if constexpr (ACT == ACT_SILU) {
         c = logistic<E>(z);
@@ -39,14 +43,22 @@ template <typename E, int ACT> __device__ __forceinline__ void act_both(float z,
     } else if constexpr (ACT == ACT_GELU) {
         normal_cdf<E>(z, c, d);
     } else {                                                        // (1 + tanh t) / 2 = logistic(2t), t = sqrt(2/pi) (z + 0.044715 z^3)
-        const float zz = z * z;
+        const float zz = zc * zc;
         c = logistic<E>(1.5957691216f * z * fmaf(0.044715f, zz, 1.f));
         d = c * (1.f - c) * (1.5957691216f * fmaf(0.134145f, zz, 1.f));
     }
-    a = c == 0.f ? 0.f : z * c;
-    slope = fabsf(z) < 1000.f ? fmaf(z, d, c) : c;
+    a = fmaxf(z, -1000.f) * c;                                      // (a NaN is one in c)
+    slope = fmaf(zc, d, c);
 }
-template <typename E, int ACT> __device__ __forceinline__ float act_only(float z) { float a, s; act_both<E, ACT>(z, a, s); return a; }
+template <typename E, int ACT> __device__ __forceinline__ float act_only(float z) {
+    float a, s;
+    if constexpr (ACT == ACT_GELU && sizeof(E) == 2) {              // z P(z) = max(z, 0) - |z| P(-|z|)
+        const float tail = normal_tail(z, s);
+        return fmaf(-fminf(fabsf(z), 1000.f), tail, fmaxf(z, 0.f));
+    }
+    act_both<E, ACT>(z, a, s);
+    return a;
+}
 
 // Two neighbouring elements in one word, rounded to nearest even (one instruction, where two conversions and a merge take four)
 template <typename E> __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
