@@ -221,7 +221,9 @@ hipError_t launch_any(const Operand& P, const Operand& Q, const GemmShape& g, co
 
 template <typename E, int EP> hipError_t with_act(const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, hipStream_t s) {
     switch (e.act) {
-        case ACT_NONE: return launch_any<E, EP, ACT_NONE, false, false>(P, Q, g, e, 1, s);
+        case ACT_NONE:
+            if constexpr (EP == EP_DLINEAR) return hipErrorInvalidValue;         // dz is dy as it stands
+            else return launch_any<E, EP, ACT_NONE, false, false>(P, Q, g, e, 1, s);
         case ACT_SILU: return launch_any<E, EP, ACT_SILU, false, false>(P, Q, g, e, 1, s);
         case ACT_GELU: return launch_any<E, EP, ACT_GELU, false, false>(P, Q, g, e, 1, s);
         case ACT_GELU_TANH: return launch_any<E, EP, ACT_GELU_TANH, false, false>(P, Q, g, e, 1, s);
@@ -230,7 +232,8 @@ template <typename E, int EP> hipError_t with_act(const Operand& P, const Operan
 }
 
 template <typename E, int EP> hipError_t with_layout(bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s) {
-    if (!pa && !qa) return launch_any<E, EP, ACT_NONE, false, false>(P, Q, g, e, nsplit, s);
+    if constexpr (EP == EP_PART)
+        if (!pa && !qa) return launch_any<E, EP, ACT_NONE, false, false>(P, Q, g, e, nsplit, s);
     if (pa && !qa) return launch_any<E, EP, ACT_NONE, true, false>(P, Q, g, e, nsplit, s);
     if (pa && qa) return launch_any<E, EP, ACT_NONE, true, true>(P, Q, g, e, nsplit, s);
     return hipErrorInvalidValue;

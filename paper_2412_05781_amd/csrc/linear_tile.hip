@@ -418,7 +418,9 @@ __device__ __forceinline__ void gemm_tile(const Operand& P, const Operand& Q, co
         finish_tile<E, EP, ACT_NONE, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split);
     } else {
         switch (e.act) {                                   // uniform
-            case ACT_NONE: finish_tile<E, EP, ACT_NONE, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split); break;
+            case ACT_NONE:
+                if constexpr (EP != EP_DLINEAR) finish_tile<E, EP, ACT_NONE, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split);
+                break;                                     // (dz is dy as it stands)
             case ACT_SILU: finish_tile<E, EP, ACT_SILU, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split); break;
             case ACT_GELU: finish_tile<E, EP, ACT_GELU, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split); break;
             default: finish_tile<E, EP, ACT_GELU_TANH, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split); break;
