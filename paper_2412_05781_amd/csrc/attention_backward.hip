@@ -23,22 +23,75 @@ template <typename E, int DP> constexpr int backward_waves() { return DP <= (siz
 // 2 x 8 x 1024 x 1024 x D (128: 2 x 8 x 2048 x 2048): D 96 57 / 58, 128 187 / 173, 160 94 / 99, 256 366 / 153 (registers spill).  fp32's tiles are too large for it.
 template <typename E, int DP> constexpr bool backward_ahead() { return sizeof(E) == 2 && (DP <= 6 || DP == 10); }
 
-// adds the accumulators of waves 2 and 3 to those of waves 0 and 1, through LDS; called by the whole workgroup
-template <int N> __device__ __forceinline__ void add_halves(float16_t (&acc)[N], unsigned char* lds, int wave, int lane) {
+// fp16 ends at 65504 and loses bits below 6e-5, and the gradients of the scores may lie beyond either where the results do not.  They become an operand times
+// f = 2^e, with an e of its own for each column of the product (a query row, or a key; one per lane, the same in both halves), and the accumulated sums carry
+// that factor too.  e falls when a value passes 2^15, to where the column's largest so far is between 2^7 and 2^8: once or twice a column.  The first e cannot take
+// a value out of fp32: |ds| < 2^42, by fp16's own range.  Softmax weights are at most 1 and take a fixed 2^12, with which 2^-26 is still a normal number.
+// Heads of more than 160 channels have no registers left for the branch: they find the largest value in a pass of its own and keep one e (2 x 8 x 1024 x 1024 x
+// 256: 233 us; 465 with the branch, which spills).  us without / with factors: 4 x 10 x 1024 x 154 x 64 33.8 / 35.1, 4 x 8 x 1024 x 1024 x 80 71 / 75,
+// 2 x 10 x 4096 x 4096 x 64 436 / 467, 2 x 8 x 2048 x 2048 x 128 171 / 186, 2 x 8 x 1024 x 1024 x 256 152 / 233.
+template <typename E> constexpr bool short_range() { return std::is_same_v<E, __half>; }
+template <typename E, int DP> constexpr bool two_passes() { return short_range<E>() && DP > 10; }
+constexpr int kWeightPower = 12;
+struct ColumnPower {
+    int e = 60;
+    float f = 0x1p60f;
+    float top = 0.f;                                       // of a pass that looks only
+    __device__ __forceinline__ void look(const float16_t& ds) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q) top = fmaxf(top, fabsf(ds[q]));
+    }
+    __device__ __forceinline__ void decide() {
+        e += 14 - __builtin_amdgcn_frexp_expf(fmaxf(top, __shfl_xor(top, 32)));
+        f = __builtin_amdgcn_ldexpf(1.f, e);
+    }
+    // ds: 16 values with the factor; `sums` the N accumulators that have it, `more` another sum.  Called by whole waves; `on` false: the column does not count
+    template <int N, int M> __device__ __forceinline__ void settle(float16_t& ds, float16_t (&sums)[M], float& more, bool on) {
+        float top = 0.f;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) top = fmaxf(top, fabsf(ds[q]));
+        if (__builtin_expect(__any(on && top > 32768.f), 0)) {
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const int down = on && top > 32768.f ? 8 - __builtin_amdgcn_frexp_expf(top) : 0;        // (infinity stays what it is)
+            const float by = __builtin_amdgcn_ldexpf(1.f, down);
+            e += down;
+            f *= by;
+            more *= by;
+#pragma unroll
+            for (int q = 0; q < 16; ++q) ds[q] *= by;
+#pragma unroll
+            for (int d = 0; d < N; ++d)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) sums[d][q] *= by;
+        }
+    }
+    __device__ __forceinline__ float inverse() const { return __builtin_amdgcn_ldexpf(1.f, -e); }
+};
+
+// accumulators times their factors, `first` for the first half of them; with two waves for the same rows (!WIDE) those of waves 2 and 3 are added to those of waves 0
+// and 1, through LDS; called by the whole workgroup
+template <bool WIDE, int N> __device__ __forceinline__ void add_halves(float16_t (&acc)[N], float first, float second, unsigned char* lds, int wave, int lane) {
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[d][q] *= 2 * d < N ? first : second;
+        return;
+    }
     float* t = reinterpret_cast<float*>(lds) + (wave & 1) * (N * 1024) + lane;
     __syncthreads();
     if (wave >= 2) {
 #pragma unroll
         for (int d = 0; d < N; ++d)
 #pragma unroll
-            for (int q = 0; q < 16; ++q) t[(d * 16 + q) * 64] = acc[d][q];
+            for (int q = 0; q < 16; ++q) t[(d * 16 + q) * 64] = acc[d][q] * (2 * d < N ? first : second);
     }
     __syncthreads();
     if (wave < 2) {
 #pragma unroll
         for (int d = 0; d < N; ++d)
 #pragma unroll
-            for (int q = 0; q < 16; ++q) acc[d][q] += t[(d * 16 + q) * 64];
+            for (int q = 0; q < 16; ++q) acc[d][q] = fmaf(acc[d][q], 2 * d < N ? first : second, t[(d * 16 + q) * 64]);
     }
 }
 
@@ -101,64 +154,87 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
     constexpr int NA = MEAN ? 2 * T::NV : T::NV;           // dq, then the mean of the keys
     float16_t acc[NA] = {};
     float rest = 0.f;
+    [[maybe_unused]] ColumnPower power;
     const float c2 = a.scale * kLog2e;
-    for (int t = 0; t < tiles; ++t) {
-        unsigned char* tk = lds + (AHEAD ? (t & 1) * 2 * T::BYTES : 0);
-        unsigned char* tv = tk + T::BYTES;
-        if (!AHEAD) {
-            sk.fetch(map, on);
-            sv.fetch(map, on);
-            __syncthreads();
-        }
-        sk.put(map, tk);
-        sv.put(map, tv);
-        __syncthreads();
-        const unsigned long long now = on;
-        if (t + 1 < tiles) {
-            on = mask.bits((t + 1) * T::ROWS, len);
-            mask.request((t + 2) * T::ROWS);
-            if (AHEAD) {
+    constexpr bool TWICE = two_passes<E, DP>();
+    static_assert(!(TWICE && AHEAD), "the first pass leaves no tile on its way");
+    auto stream = [&](auto look) {                         // all tiles; look: for the largest gradient of a score only
+        for (int t = 0; t < tiles; ++t) {
+            unsigned char* tk = lds + (AHEAD ? (t & 1) * 2 * T::BYTES : 0);
+            unsigned char* tv = tk + T::BYTES;
+            if (!AHEAD) {
                 sk.fetch(map, on);
                 sv.fetch(map, on);
+                __syncthreads();
             }
-        }
+            sk.put(map, tk);
+            sv.put(map, tv);
+            __syncthreads();
+            const unsigned long long now = on;
+            if (t + 1 < tiles) {
+                on = mask.bits((t + 1) * T::ROWS, len);
+                mask.request((t + 2) * T::ROWS);
+                if (AHEAD) {
+                    sk.fetch(map, on);
+                    sv.fetch(map, on);
+                }
+            }
 #pragma unroll 1
-        for (int h = sub; h < (WIDE ? 2 : sub + 1); ++h) {
-            const uint32_t cur = (uint32_t)(now >> (32 * h));
-            if (cur == 0) continue;                        // uniform over the wave
-            float16_t s = {}, dp = {};
+            for (int h = sub; h < (WIDE ? 2 : sub + 1); ++h) {
+                const uint32_t cur = (uint32_t)(now >> (32 * h));
+                if (cur == 0) continue;                        // uniform over the wave
+                float16_t s = {}, dp = {};
 #pragma unroll
-            for (int ks = 0; ks < T::KS; ++ks) {
-                Mma<E>::run(T::along(tk, 32 * h, ks, places), fq[ks], s);
-                Mma<E>::run(T::along(tv, 32 * h, ks, places), fo[ks], dp);
-            }
+                for (int ks = 0; ks < T::KS; ++ks) {
+                    Mma<E>::run(T::along(tk, 32 * h, ks, places), fq[ks], s);
+                    Mma<E>::run(T::along(tv, 32 * h, ks, places), fo[ks], dp);
+                }
 #pragma unroll
-            for (int q = 0; q < 16; ++q) s[q] = __builtin_amdgcn_exp2f(fmaf(s[q], c2, -lse2));
-            if (cur != 0xffffffffu) {
-                asm volatile("" ::: "memory");             // a branch
-                const uint32_t mine = cur >> (4 * half);
+                for (int q = 0; q < 16; ++q) s[q] = __builtin_amdgcn_exp2f(fmaf(s[q], c2, -lse2));
+                if (cur != 0xffffffffu) {
+                    asm volatile("" ::: "memory");             // a branch
+                    const uint32_t mine = cur >> (4 * half);
 #pragma unroll
-                for (int q = 0; q < 16; ++q)
-                    if (!((mine >> (8 * (q / 4) + q % 4)) & 1)) s[q] = 0.f;
-            }
+                    for (int q = 0; q < 16; ++q)
+                        if (!((mine >> (8 * (q / 4) + q % 4)) & 1)) s[q] = 0.f;
+                }
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-                dp[q] = s[q] * (dp[q] - dlt);
-                if constexpr (MEAN) rest += dp[q];
-            }
+                for (int q = 0; q < 16; ++q) {
+                    if constexpr (short_range<E>()) dp[q] = s[q] * fmaf(dp[q], power.f, -dlt * power.f);
+                    else dp[q] = s[q] * (dp[q] - dlt);
+                    if constexpr (MEAN && !look) rest += dp[q];
+                }
+                if constexpr (look) {
+                    power.look(dp);
+                    continue;
+                }
+                if constexpr (short_range<E>() && !TWICE) power.settle<T::NV>(dp, acc, rest, true);
 #pragma unroll
-            for (int st = 0; st < T::ST; ++st) {
-                const u32x4_t w = T::weights(dp, st), wp = MEAN ? T::weights(s, st) : w;
+                for (int st = 0; st < T::ST; ++st) {
+                    const u32x4_t w = T::weights(dp, st), wp = MEAN ? T::weights(s, st) : w;
 #pragma unroll
-                for (int d = 0; d < T::NV; ++d) {
-                    const u32x4_t keys = T::across(tk, 32 * h, st, d, places);
-                    Mma<E>::run(keys, w, acc[d]);
-                    if constexpr (MEAN) Mma<E>::run(keys, wp, acc[T::NV + d]);
+                    for (int d = 0; d < T::NV; ++d) {
+                        const u32x4_t keys = T::across(tk, 32 * h, st, d, places);
+                        Mma<E>::run(keys, w, acc[d]);
+                        if constexpr (MEAN) Mma<E>::run(keys, wp, acc[T::NV + d]);
+                    }
                 }
             }
         }
+    };
+    if constexpr (TWICE) {
+        stream(std::true_type());
+        power.decide();
+        sk.jump(-tiles * sk.step);
+        sv.jump(-tiles * sv.step);
+        mask.request(0);
+        on = mask.bits(0, len);
+        mask.request(T::ROWS);
     }
-    if constexpr (!WIDE) add_halves<NA>(acc, lds, wave, lane);
+    stream(std::false_type());
+    const float back = short_range<E>() ? power.inverse() : 1.f;
+    rest *= back;
+    add_halves<WIDE>(acc, back, 1.f, lds, wave, lane);
     if constexpr (MEAN) {
         rest += __shfl_xor(rest, 32);
         if constexpr (!WIDE) {
@@ -207,13 +283,16 @@ attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit,
     if (__syncthreads_or(key_on)) {
         const int head_tiles = (a.Sq + T::ROWS - 1) / T::ROWS, tiles = G * head_tiles;
         const int t0 = (int)((long long)split * tiles / nsplit), t1 = (int)((long long)(split + 1) * tiles / nsplit);
-        int g = t0 / head_tiles, ht = t0 - g * head_tiles;                           // head and tile of the next fetch
+        const int g0 = t0 / head_tiles, ht0 = t0 - g0 * head_tiles;
+        int g = g0, ht = ht0;                                                        // head and tile of the next fetch
         using Stream = AttnStream<E, DP>;
         const typename Stream::Map map(tid, a.D);
         const unsigned char* qbase = static_cast<const unsigned char*>(a.q.p) + ((long long)b * a.q.b + (long long)(hk * G + g) * a.q.h) * T::ES;
         const unsigned char* obase = static_cast<const unsigned char*>(a.dout.p) + ((long long)b * a.dout.b + (long long)(hk * G + g) * a.dout.h) * T::ES;
         Stream sq(map, qbase, (long long)ht * T::ROWS, a.q.s), so(map, obase, (long long)ht * T::ROWS, a.dout.s);
         float nlse = 0.f, dlt = 0.f;
+        constexpr float lift = short_range<E>() ? kWeightPower : 0.f;                // weights times 2^lift, and with them the gradients of the scores
+        [[maybe_unused]] ColumnPower power;
         auto fetch = [&] {
             const int left = a.Sq - ht * T::ROWS;
             const unsigned long long on = left >= T::ROWS ? ~0ull : (1ull << left) - 1;
@@ -221,7 +300,7 @@ attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit,
             so.fetch(map, on);
             if (tid < T::ROWS) {
                 const long long at = ((long long)bh * G + g) * a.Sq + ht * T::ROWS + tid;
-                nlse = tid < left ? -a.lse[at] * kLog2e : -INFINITY;                 // a row behind the last: p = 0
+                nlse = tid < left ? fmaf(-a.lse[at], kLog2e, lift) : -INFINITY;         // a row behind the last: p = 0
                 dlt = tid < left ? parts.delta[at] : 0.f;
             }
             if (++ht == head_tiles) {
@@ -243,52 +322,72 @@ attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit,
             }
         }
         const float c2 = a.scale * kLog2e;
-        for (int t = t0; t < t1; ++t) {
-            const int buffer = AHEAD ? (t - t0) & 1 : 0;
-            unsigned char* tq = lds + buffer * 2 * T::BYTES;
-            unsigned char* to = tq + T::BYTES;
-            float* tl = stats + buffer * 2 * T::ROWS;
-            float* td = tl + T::ROWS;
-            if (!AHEAD) {
-                fetch();
+        constexpr bool TWICE = two_passes<E, DP>();
+        static_assert(!(TWICE && AHEAD), "the first pass leaves no tile on its way");
+        auto stream = [&](auto look) {                     // as above
+            for (int t = t0; t < t1; ++t) {
+                const int buffer = AHEAD ? (t - t0) & 1 : 0;
+                unsigned char* tq = lds + buffer * 2 * T::BYTES;
+                unsigned char* to = tq + T::BYTES;
+                float* tl = stats + buffer * 2 * T::ROWS;
+                float* td = tl + T::ROWS;
+                if (!AHEAD) {
+                    fetch();
+                    __syncthreads();
+                }
+                sq.put(map, tq);
+                so.put(map, to);
+                if (tid < T::ROWS) { tl[tid] = nlse; td[tid] = dlt; }
                 __syncthreads();
-            }
-            sq.put(map, tq);
-            so.put(map, to);
-            if (tid < T::ROWS) { tl[tid] = nlse; td[tid] = dlt; }
-            __syncthreads();
-            if (AHEAD && t + 1 < t1) fetch();
+                if (AHEAD && t + 1 < t1) fetch();
 #pragma unroll 1
-            for (int h = sub; h < (WIDE ? 2 : sub + 1); ++h) {
-                float16_t s = {}, dp = {};
+                for (int h = sub; h < (WIDE ? 2 : sub + 1); ++h) {
+                    float16_t s = {}, dp = {};
 #pragma unroll
-                for (int ks = 0; ks < T::KS; ++ks) {
-                    Mma<E>::run(T::along(tq, 32 * h, ks, places), fk[ks], s);
-                    Mma<E>::run(T::along(to, 32 * h, ks, places), fv[ks], dp);
-                }
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float4 nl = *reinterpret_cast<const float4*>(tl + 32 * h + 8 * q + 4 * half), dl = *reinterpret_cast<const float4*>(td + 32 * h + 8 * q + 4 * half);
-                    const float n4[4] = {nl.x, nl.y, nl.z, nl.w}, d4[4] = {dl.x, dl.y, dl.z, dl.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * q + j], c2, n4[j]));
-                        s[4 * q + j] = p;
-                        dp[4 * q + j] = p * (dp[4 * q + j] - d4[j]);
+                    for (int ks = 0; ks < T::KS; ++ks) {
+                        Mma<E>::run(T::along(tq, 32 * h, ks, places), fk[ks], s);
+                        Mma<E>::run(T::along(to, 32 * h, ks, places), fv[ks], dp);
                     }
-                }
 #pragma unroll
-                for (int st = 0; st < T::ST; ++st) {
-                    const u32x4_t wp = T::weights(s, st), wd = T::weights(dp, st);
+                    for (int q = 0; q < 4; ++q) {
+                        const float4 nl = *reinterpret_cast<const float4*>(tl + 32 * h + 8 * q + 4 * half), dl = *reinterpret_cast<const float4*>(td + 32 * h + 8 * q + 4 * half);
+                        const float n4[4] = {nl.x, nl.y, nl.z, nl.w}, d4[4] = {dl.x, dl.y, dl.z, dl.w};
 #pragma unroll
-                    for (int d = 0; d < T::NV; ++d) {
-                        Mma<E>::run(T::across(to, 32 * h, st, d, places), wp, acc[T::NV + d]);
-                        Mma<E>::run(T::across(tq, 32 * h, st, d, places), wd, acc[d]);
+                        for (int j = 0; j < 4; ++j) {
+                            const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * q + j], c2, n4[j]));
+                            s[4 * q + j] = p;
+                            dp[4 * q + j] = (short_range<E>() ? p * power.f : p) * (dp[4 * q + j] - d4[j]);
+                        }
+                    }
+                    if constexpr (look) {
+                        power.look(dp);
+                        continue;
+                    }
+                    float none = 0.f;
+                    if constexpr (short_range<E>() && !TWICE) power.settle<T::NV>(dp, acc, none, key_on);
+#pragma unroll
+                    for (int st = 0; st < T::ST; ++st) {
+                        const u32x4_t wp = T::weights(s, st), wd = T::weights(dp, st);
+#pragma unroll
+                        for (int d = 0; d < T::NV; ++d) {
+                            Mma<E>::run(T::across(to, 32 * h, st, d, places), wp, acc[T::NV + d]);
+                            Mma<E>::run(T::across(tq, 32 * h, st, d, places), wd, acc[d]);
+                        }
                     }
                 }
             }
+        };
+        if constexpr (TWICE) {
+            stream(std::true_type());
+            power.decide();
+            sq.jump((ht0 - ht) * sq.step + (long long)(g0 - g) * a.q.h * T::ES);
+            so.jump((ht0 - ht) * so.step + (long long)(g0 - g) * a.dout.h * T::ES);
+            g = g0;
+            ht = ht0;
         }
-        if constexpr (!WIDE) add_halves<2 * T::NV>(acc, lds, wave, lane);
+        stream(std::false_type());
+        constexpr float drop = short_range<E>() ? 1.f / (1 << kWeightPower) : 1.f;
+        add_halves<WIDE>(acc, short_range<E>() ? power.inverse() * drop : 1.f, drop, lds, wave, lane);
     }
     if (sub || !in_range) return;
     if (!key_on) {
