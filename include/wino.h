@@ -371,8 +371,9 @@ int wino_i8_batched_gemm(const void *Uq, const float *dU, const void *Vq, const 
  * determinism and errors as above.  Sums, softmax statistics and bias gradients are fp32; a result is rounded once to `dtype`.
  * Where a call needs more than one kernel, what passes between them is in fp32, except the gradient of the pre-activations (dz,
  * [du | dg] below).  That, and the softmax weights and their gradients inside the attention kernels, are operands of the next matrix
- * product and are rounded to `dtype` for it.  (fp16: the gradients of the softmax scores are rounded times a power of two of each query
- * row or key, so that only what the results themselves cannot hold is lost to the type's range.)  Attention and, with two-byte types, the activations take the hardware's exponential
+ * product and are rounded to `dtype` for it.  (fp16: the gradients of the pre-activations times a power of two of the call where their
+ * largest finite one is below 1 or beyond 65504, those of the softmax scores times one of each query row or key, so that only what the
+ * results themselves cannot hold is lost to the type's range.)  Attention and, with two-byte types, the activations take the hardware's exponential
  * and reciprocal (one unit in the last place of fp32); the activations of fp32 calls take the library's functions.
  * "Overlap" is taken from the first to the last byte of a tensor, gaps between strided rows included.
  * A workspace belongs to one call at a time: calls on different streams, and graphs that may run at the same time, need one each.

@@ -37,26 +37,28 @@ hipError_t product(int ep, bool pt, bool qt, const Operand& P, const Operand& Q,
     return rc != hipSuccess ? rc : launch_join(e.part, n, g, e, dt, s);
 }
 
-// workspace of a backward pass over W output columns: dz, the column sums, the ranges' sums
-struct BackwardSpace { size_t dz, sums, parts, total; long long ld; int sum_rows; };
-BackwardSpace backward_space(int M, int W, int K, int dt, bool stored) {
+// workspace of a backward pass over W output columns (`halves` of them a column of dy): dz, the column sums, the ranges' sums; fp16: the largest of dz by wave and their power
+struct BackwardSpace { size_t dz, sums, parts, tops, total; long long ld; Filled filled; };
+BackwardSpace backward_space(int M, int W, int K, int dt, bool stored, int halves) {
     BackwardSpace b;
     b.ld = ((long long)W + 7) / 8 * 8;
     b.dz = stored ? up256((size_t)M * b.ld * bytes_of(dt)) : 0;
-    b.sum_rows = stored ? gemm_most_sum_rows(M) : column_sum_rows(M);
-    b.sums = up256((size_t)b.sum_rows * W * sizeof(float));
+    b.filled = Filled{stored ? gemm_most_sum_rows(M) : column_sum_rows(M), stored && dt == WINO_F16 ? gemm_most_tops(M, W / halves) : 0};
+    b.sums = up256((size_t)b.filled.sum_rows * W * sizeof(float));
     b.parts = product_bytes(M, K, W, dt) + product_bytes(W, K, M, dt);
-    b.total = b.dz + b.sums + b.parts;
+    b.tops = b.filled.tops ? 256 + up256((size_t)b.filled.tops * sizeof(float)) : 0;
+    b.total = b.dz + b.sums + b.parts + b.tops;
     return b;
 }
 
 // dx = dz w and dw = dz^T x, in one launch where both are asked for; and the column sums of dz
-int run_products(const void* x, long long ldx, const void* w, const void* dz, long long lddz, void* dx, long long lddx, void* dw, const ColumnSums& c, int M, int W, int K,
-                 void* scratch, int dt, hipStream_t s) {
+int run_products(const void* x, long long ldx, const void* w, const void* dz, long long lddz, void* dx, long long lddx, void* dw, const ColumnSums& c, const int* power,
+                 int M, int W, int K, void* scratch, int dt, hipStream_t s) {
     Product a{Operand{w, K}, Operand{dz, lddz}, GemmShape{M, K, W}, Epilogue(), gemm_ranges(M, K, W, dt)};
     Product b{Operand{x, ldx}, Operand{dz, lddz}, GemmShape{W, K, M}, Epilogue(), gemm_ranges(W, K, M, dt)};
     a.e.out = dx; a.e.ld_out = lddx;
     b.e.out = dw; b.e.ld_out = K;
+    a.e.power = b.e.power = power;
     if ((!dx || !dw) && c.out && launch_column_sums(c, dt, s) != hipSuccess) return WINO_ERR_HIP;
     if (!dx && !dw) return WINO_OK;
     if (!dw) return product(EP_STORE, true, false, a.P, a.Q, a.g, a.e, scratch, dt, s) == hipSuccess ? WINO_OK : WINO_ERR_HIP;
@@ -93,7 +95,7 @@ int products_backward(const void* x, const void* w, const float* bias, const voi
         for (int j = 0; j < i; ++j) if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return WINO_ERR_ALIAS;
     }
     const bool stored = halves == 2 || act != WINO_ACT_NONE;
-    BackwardSpace b = backward_space(M, W, K, dt, stored);
+    BackwardSpace b = backward_space(M, W, K, dt, stored, halves);
     if (!workspace || workspace_bytes < b.total) return WINO_ERR_WORKSPACE;
     if (!at16(workspace)) return WINO_ERR_ALIGN;
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -101,19 +103,30 @@ int products_backward(const void* x, const void* w, const float* bias, const voi
     float* sums = reinterpret_cast<float*>(base + b.dz);
     const void* dz = dy;
     long long lddz = lddy;
-    ColumnSums c{dy, lddy, M, N, nullptr, b.sum_rows, false};
+    ColumnSums c{dy, lddy, M, N, nullptr, b.filled.sum_rows, false};
+    int* power = nullptr;
     if (stored) {
         Epilogue e;
         e.bias = bias; e.extra = dy; e.ld_extra = lddy; e.out = base; e.ld_out = b.ld; e.sums = sums; e.act = act;
-        if (launch_gemm(halves == 2 ? EP_DGLU : EP_DLINEAR, false, false, Operand{w, K}, Operand{x, ldx}, GemmShape{M, N, K}, e, 1, dt, s, &b.sum_rows) != hipSuccess) return WINO_ERR_HIP;
+        const int ep = halves == 2 ? EP_DGLU : EP_DLINEAR;
+        if (b.tops && (dx || dw)) {
+            power = reinterpret_cast<int*>(base + b.dz + b.sums + b.parts);
+            e.tops = reinterpret_cast<float*>(power) + 64;
+        }
+        if (launch_gemm(ep, false, false, Operand{w, K}, Operand{x, ldx}, GemmShape{M, N, K}, e, 1, dt, s, &b.filled) != hipSuccess) return WINO_ERR_HIP;
+        if (power) {
+            if (launch_power(e.tops, b.filled.tops, power, s) != hipSuccess) return WINO_ERR_HIP;
+            e.tops = nullptr; e.power = power;
+            if (launch_gemm(ep, false, false, Operand{w, K}, Operand{x, ldx}, GemmShape{M, N, K}, e, 1, dt, s) != hipSuccess) return WINO_ERR_HIP;
+        }
         dz = base; lddz = b.ld;
-        if (dbias) c = ColumnSums{sums, W, b.sum_rows, W, dbias, 1, true};
+        if (dbias) c = ColumnSums{sums, W, b.filled.sum_rows, W, dbias, 1, true};
     } else if (dbias) {
-        c.out = b.sum_rows == 1 ? dbias : sums;
+        c.out = b.filled.sum_rows == 1 ? dbias : sums;
     }
-    const int rc = run_products(x, ldx, w, dz, lddz, dx, lddx, dw, c, M, W, K, base + b.dz + b.sums, dt, s);
+    const int rc = run_products(x, ldx, w, dz, lddz, dx, lddx, dw, c, power, M, W, K, base + b.dz + b.sums, dt, s);
     if (rc != WINO_OK || !dbias || c.out == dbias) return rc;
-    return launch_sum_rows(sums, b.sum_rows, W, dbias, s) == hipSuccess ? WINO_OK : WINO_ERR_HIP;
+    return launch_sum_rows(sums, b.filled.sum_rows, W, dbias, s) == hipSuccess ? WINO_OK : WINO_ERR_HIP;
 }
 
 // ---- attention ------------------------------------------------------------------------------------------------------------------------
@@ -274,7 +287,7 @@ int wino_linear(const void* x, const void* w, const float* bias, const void* res
 
 size_t wino_linear_backward_workspace_bytes(int M, int N, int K, int dtype, int act) {
     if (!is_dtype(dtype) || !is_act(act) || !product_dims_ok(M, N, K, 1)) return 0;
-    return backward_space(M, N, K, dtype, act != WINO_ACT_NONE).total;
+    return backward_space(M, N, K, dtype, act != WINO_ACT_NONE, 1).total;
 }
 
 int wino_linear_backward(const void* x, const void* w, const float* bias, const void* dy, void* dx, void* dw, float* dbias, int M, int N, int K, long long ldx,
@@ -305,7 +318,7 @@ int wino_glu(const void* x, const void* w, const float* bias, void* h, int M, in
 
 size_t wino_glu_backward_workspace_bytes(int M, int N, int K, int dtype, int act) {
     if (!is_dtype(dtype) || !is_act(act) || !product_dims_ok(M, N, K, 2)) return 0;
-    return backward_space(M, 2 * N, K, dtype, true).total;
+    return backward_space(M, 2 * N, K, dtype, true, 2).total;
 }
 
 int wino_glu_backward(const void* x, const void* w, const float* bias, const void* dh, void* dx, void* dw, float* dbias, int M, int N, int K, long long ldx,

@@ -33,8 +33,14 @@ struct Epilogue {
     long long ld_out = 0;
     float* sums = nullptr;           // [sum_rows][width of out]
     float* part = nullptr;           // [nsplit][M][N]
+    float* tops = nullptr;           // EP_DLINEAR / EP_DGLU in fp16: the largest finite magnitude of out (before its rounding), by wave; may be null
+    const int* power = nullptr;      // EP_DLINEAR / EP_DGLU in fp16: out is formed again times 2^*power, or left alone where that is 0.  EP_STORE and joins: result
+                                     // times 2^-*power.  May be null
     int act = ACT_NONE;
 };
+
+// how many rows of sums and how many tops a launch with EP_DLINEAR / EP_DGLU fills
+struct Filled { int sum_rows; long long tops; };
 
 // M rows and N columns of out (EP_GLU / EP_DGLU: N gate pairs, P has 2N rows), reduction length K.
 struct GemmShape { int M, N, K; };
@@ -43,12 +49,13 @@ struct GemmShape { int M, N, K; };
 struct Product { Operand P, Q; GemmShape g; Epilogue e; int nsplit; };
 
 bool gemm_dims_ok(long long M, long long N, long long K);
-// rows of Epilogue::sums that a launch with EP_DLINEAR / EP_DGLU may fill; launch_gemm says how many it did (sum_rows, may be null)
+// rows of Epilogue::sums and number of Epilogue::tops that a launch with EP_DLINEAR / EP_DGLU may fill; launch_gemm says how many it did (may be null)
 int gemm_most_sum_rows(int M);
+long long gemm_most_tops(int M, int N);
 // ranges the reduction of a plain product (EP_STORE, EP_LINEAR) is cut into
 int gemm_ranges(int M, int N, int K, int dt);
 hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit,
-                       int dt, hipStream_t s, int* sum_rows = nullptr);
+                       int dt, hipStream_t s, Filled* filled = nullptr);
 // Sums over the rows of x[M][N], in `ranges` ranges: out[range][n].  out null: not asked for.  f32: x is fp32 whatever the call's type, in one range.
 struct ColumnSums { const void* x; long long ld; int M, N; float* out; int ranges; bool f32; };
 // a = dz w (P across, Q along the reduction) and b = dz^T x (both across), with EP_STORE or ranges; and the column sums c
@@ -60,6 +67,8 @@ hipError_t launch_few_gemm(bool glu, const Operand& P, const Operand& Q, const G
 hipError_t launch_join(const float* part, int nsplit, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s);
 // out[c] = sum over rows of part[row][c]
 hipError_t launch_sum_rows(const float* part, int rows, int cols, float* out, hipStream_t s);
+// the power of two for an fp16 tensor whose largest finite magnitude is the largest of `tops`: 0 where it fits and keeps its bits as it is
+hipError_t launch_power(const float* tops, long long n, int* power, hipStream_t s);
 int column_sum_rows(int M);
 hipError_t launch_column_sums(const ColumnSums& c, int dt, hipStream_t s);
 

@@ -12,12 +12,15 @@ namespace wino {
 namespace {
 
 // four columns n0.. of row m, from the sums of one lane; returns in c (and c2: the gate half) what the column sums take
+// f: the power of two that what is stored takes (EP_STORE, EP_DLINEAR, EP_DGLU)
 template <typename E, int EP, int ACT>
-__device__ __forceinline__ void finish4(const GemmShape& g, const Epilogue& e, long long m, int n0, const float* s, const float* s2, float* c, float* c2) {
+__device__ __forceinline__ void finish4(const GemmShape& g, const Epilogue& e, long long m, int n0, const float* s, const float* s2, float* c, float* c2, float f) {
     const int n = g.N - n0;
     float a[4];
     if constexpr (EP == EP_STORE) {
-        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = s[i] * f;
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, a);
     } else if constexpr (EP == EP_LINEAR) {
         float r[4] = {0.f, 0.f, 0.f, 0.f};
         if (e.extra) load4<E>(static_cast<const E*>(e.extra) + m * e.ld_extra + n0, n, r);
@@ -36,8 +39,9 @@ __device__ __forceinline__ void finish4(const GemmShape& g, const Epilogue& e, l
             float v, d;
             act_both<E, ACT>(s[i] + b, v, d);
             c[i] = i < n ? r[i] * d : 0.f;
+            a[i] = c[i] * f;
         }
-        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, c);
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, a);
     } else if constexpr (EP == EP_GLU) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -55,9 +59,12 @@ __device__ __forceinline__ void finish4(const GemmShape& g, const Epilogue& e, l
             act_both<E, ACT>(s2[i] + bg, v, d);
             c[i] = i < n ? r[i] * v : 0.f;
             c2[i] = i < n ? r[i] * (s[i] + bu) * d : 0.f;
+            a[i] = c[i] * f;
         }
-        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, c);
-        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + g.N + n0, n, c2);
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + n0, n, a);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = c2[i] * f;
+        store4<E>(static_cast<E*>(e.out) + m * e.ld_out + g.N + n0, n, a);
     }
 }
 
@@ -82,6 +89,9 @@ __global__ void __launch_bounds__(256) gemm_any_kernel(Operand P, Operand Q, Gem
 
     const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if (logical >= total) return;                          // uniform per workgroup, before any barrier
+    constexpr bool SUMS = EP == EP_DLINEAR || EP == EP_DGLU;
+    const float factor = store_factor<E, SUMS>(e);
+    if (SUMS && factor == 0.f) return;                     // nothing to do again
     const int split = logical / (tiles_p * tiles_q), in = logical - split * (tiles_p * tiles_q);
     const int bq = in / tiles_p, bp = in - bq * tiles_p;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wp = wave & 1, wq = wave >> 1;
@@ -181,7 +191,7 @@ __global__ void __launch_bounds__(256) gemm_any_kernel(Operand P, Operand Q, Gem
             }
         return;
     }
-    constexpr bool SUMS = EP == EP_DLINEAR || EP == EP_DGLU;
+    float top = 0.f;
 #pragma unroll
     for (int i = 0; i < (GLU ? 1 : 2); ++i)
 #pragma unroll
@@ -190,8 +200,13 @@ __global__ void __launch_bounds__(256) gemm_any_kernel(Operand P, Operand Q, Gem
             float s[4], s2[4], c[4] = {}, c2[4] = {};
 #pragma unroll
             for (int j = 0; j < 4; ++j) { s[j] = acc[i][4 * q + j]; s2[j] = acc[1][4 * q + j]; }
-            if (m < g.M && n < g.N) finish4<E, EP, ACT>(g, e, m, n, s, s2, c, c2);
+            if (m < g.M && n < g.N) finish4<E, EP, ACT>(g, e, m, n, s, s2, c, c2, factor);
             if constexpr (SUMS) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    top = larger_finite(top, c[j]);
+                    if constexpr (EP == EP_DGLU) top = larger_finite(top, c2[j]);
+                }
                 const long long row = (long long)bq * 2 + wq;
                 const int width = EP == EP_DGLU ? 2 * g.N : g.N;
 #pragma unroll
@@ -205,6 +220,7 @@ __global__ void __launch_bounds__(256) gemm_any_kernel(Operand P, Operand Q, Gem
                 }
             }
         }
+    if constexpr (SUMS && std::is_same_v<E, __half>) store_top(e, ((long long)bq * tiles_p + bp) * 4 + wave, top, lane);
 }
 
 template <typename E, int EP, int ACT, bool PA, bool QA>
@@ -243,6 +259,7 @@ template <typename E, int EP> hipError_t with_layout(bool pa, bool qa, const Ope
 template <typename E, int ACT> __global__ void __launch_bounds__(256) join_kernel(const float* part, int nsplit, GemmShape g, Epilogue e, bool linear) {
     const long long quads = (g.N + 3) / 4, id = (long long)blockIdx.x * 256 + threadIdx.x;
     if (id >= quads * g.M) return;
+    const float factor = store_factor<E, false>(e);
     const long long m = id / quads;
     const int n0 = (int)(id - m * quads) * 4;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
@@ -260,8 +277,8 @@ template <typename E, int ACT> __global__ void __launch_bounds__(256) join_kerne
             for (int i = 0; i < 4; ++i)
                 if (n0 + i < g.N) s[i] += p[(size_t)r * step + i];
     }
-    if (linear) finish4<E, EP_LINEAR, ACT>(g, e, m, n0, s, s, nullptr, nullptr);
-    else finish4<E, EP_STORE, ACT>(g, e, m, n0, s, s, nullptr, nullptr);
+    if (linear) finish4<E, EP_LINEAR, ACT>(g, e, m, n0, s, s, nullptr, nullptr, factor);
+    else finish4<E, EP_STORE, ACT>(g, e, m, n0, s, s, nullptr, nullptr, factor);
 }
 
 // 64 columns per workgroup, sixteen waves that take every sixteenth row
@@ -282,6 +299,21 @@ __global__ void __launch_bounds__(1024) sum_rows_kernel(const float* part, int r
     }
 }
 
+// Up to 65504 there is nothing to do, and from 1 on what lies a factor of 2^14 below the largest still has all its bits.  Otherwise the largest goes to 2^14 .. 2^15.
+__global__ void __launch_bounds__(1024) power_kernel(const float* tops, long long n, int* power) {
+    __shared__ float t[16];
+    float v = 0.f;
+    for (long long i = threadIdx.x; i < n; i += 1024) v = fmaxf(v, tops[i]);
+    v = wave_max(v);
+    if ((threadIdx.x & 63) == 0) t[threadIdx.x >> 6] = v;
+    __syncthreads();
+    if (threadIdx.x) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) v = fmaxf(v, t[i]);
+    const int p = 15 - __builtin_amdgcn_frexp_expf(v);
+    *power = v == 0.f || (v >= 1.f && v <= 65504.f) ? 0 : p < 100 ? p : 100;
+}
+
 template <typename E> __global__ void __launch_bounds__(256) column_sums_kernel(ColumnSums c, bool vec) {
     __shared__ float t[4 * 64];
     column_sums<E, 4>(c, vec, blockIdx.x, blockIdx.y, gridDim.y, t);
@@ -297,6 +329,9 @@ bool gemm_dims_ok(long long M, long long N, long long K) {
 
 // one row of sums per 32 rows, per 64 rows twice, per 128 rows twice or four times, or per 256 rows four times
 int gemm_most_sum_rows(int M) { return (M + 63) / 64 * 2 + 4; }
+
+// four for a tile of 64 x 64 or more, eight for one of twice that or more
+long long gemm_most_tops(int M, int N) { return 4 * (((long long)M + 63) / 64 + 1) * (((long long)N + 63) / 64 + 1); }
 
 // How many ranges a reduction is cut into: the number with the least time by this count.  A stage of a 64x64 tile takes a workgroup 0.29 us where it waits
 // for its operands (two-byte types, up to 768 workgroups side by side: 512 x 5120 x 1280, 160 tiles, 23 us) and 0.49 us of a compute unit's MFMAs for
@@ -320,9 +355,13 @@ int gemm_ranges(int M, int N, int K, int dt) {
 }
 
 hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, int dt, hipStream_t s,
-                       int* sum_rows) {
-    if (tile_gemm_ok(ep, p_trans, q_trans, P, Q, g, e, dt)) return launch_tile_gemm(ep, p_trans, q_trans, P, Q, g, e, nsplit, dt, s, sum_rows);
-    if (sum_rows) *sum_rows = (g.M + kBQ - 1) / kBQ * 2;
+                       Filled* filled) {
+    if (tile_gemm_ok(ep, p_trans, q_trans, P, Q, g, e, dt)) return launch_tile_gemm(ep, p_trans, q_trans, P, Q, g, e, nsplit, dt, s, filled);
+    if (filled) {
+        const int bn = ep == EP_DGLU ? kBP / 2 : kBP;
+        filled->sum_rows = (g.M + kBQ - 1) / kBQ * 2;
+        filled->tops = 4LL * ((g.M + kBQ - 1) / kBQ) * ((g.N + bn - 1) / bn);
+    }
     return with_dtype(dt, [&](auto* tag) -> hipError_t {
         using E = std::remove_pointer_t<decltype(tag)>;
         switch (ep) {
@@ -364,6 +403,11 @@ hipError_t launch_join(const float* part, int nsplit, const GemmShape& g, const 
 
 hipError_t launch_sum_rows(const float* part, int rows, int cols, float* out, hipStream_t s) {
     hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, s, part, rows, cols, out);
+    return hipGetLastError();
+}
+
+hipError_t launch_power(const float* tops, long long n, int* power, hipStream_t s) {
+    hipLaunchKernelGGL(power_kernel, dim3(1), dim3(1024), 0, s, tops, n, power);
     return hipGetLastError();
 }
 

@@ -57,13 +57,16 @@ template <typename E> __device__ __forceinline__ void store8(E* p, const float* 
 // Epilogue of one wave's tile.  acc[i][j]: rows n of 32-row block i (GLU: block i of the up rows, FP / 2 + i of the gate rows), columns m of block j.
 // What a block reads besides its sums is requested for all of its columns before the first is used, from clamped places; only stores are guarded.
 template <typename E, int EP, int ACT, int FP, int FQ, int WP, int WQ>
-__device__ __forceinline__ void finish_tile(const GemmShape& g, const Epilogue& e, float16_t (&acc)[FP][FQ], int n0, long long m0, int wp, int wq, long long sum_row, int lane, int split) {
+__device__ __forceinline__ void finish_tile(const GemmShape& g, const Epilogue& e, float16_t (&acc)[FP][FQ], int n0, long long m0, int wp, int wq, long long sum_row, long long top_at, int lane, int split) {
     constexpr bool GLU = EP == EP_GLU || EP == EP_DGLU, SUMS = EP == EP_DLINEAR || EP == EP_DGLU;
     constexpr int NI = GLU ? FP / 2 : FP;
     const int half = lane >> 5;
     E* out = static_cast<E*>(e.out);
     const E* extra = static_cast<const E*>(e.extra);
     const bool has_bias = EP != EP_STORE && e.bias, has_extra = SUMS || (EP == EP_LINEAR && extra);
+    constexpr bool F16 = std::is_same_v<E, __half>;
+    const float factor = store_factor<E, SUMS>(e);
+    float top = 0.f;
     long long mrow[FQ];
     bool m_on[FQ];
 #pragma unroll
@@ -126,7 +129,7 @@ __device__ __forceinline__ void finish_tile(const GemmShape& g, const Epilogue& 
                 unpack8<E>(ex[qp][j], r);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    if constexpr (EP == EP_STORE) a[k] = s[k];
+                    if constexpr (EP == EP_STORE) a[k] = F16 ? s[k] * factor : s[k];
                     else if constexpr (EP == EP_LINEAR) a[k] = act_only<E, ACT>(s[k] + bias[qp][k]) + r[k];
                     else if constexpr (EP == EP_GLU) a[k] = (s[k] + bias[qp][k]) * act_only<E, ACT>(s2[k] + bias2[qp][k]);
                     else {
@@ -139,8 +142,16 @@ __device__ __forceinline__ void finish_tile(const GemmShape& g, const Epilogue& 
                             a[k] = r[k] * v;
                             b[k] = r[k] * (s[k] + bias[qp][k]) * d;
                             sum2[k] += on ? b[k] : 0.f;
+                            if constexpr (F16) {
+                                top = larger_finite(top, on ? b[k] : 0.f);
+                                b[k] *= factor;
+                            }
                         }
                         sum[k] += on ? a[k] : 0.f;
+                        if constexpr (F16) {
+                            top = larger_finite(top, on ? a[k] : 0.f);
+                            a[k] *= factor;
+                        }
                     }
                 }
                 if (on) {
@@ -171,6 +182,7 @@ __device__ __forceinline__ void finish_tile(const GemmShape& g, const Epilogue& 
             }
         }
     }
+    if constexpr (SUMS && F16) store_top(e, top_at, top, lane);
 }
 
 // ---- fragments under explicit control: the reads are issued from inline assembly, waited for by count, and tied to the wait by pin ----------------
@@ -413,17 +425,17 @@ __device__ __forceinline__ void gemm_tile(const Operand& P, const Operand& Q, co
         slot = next_slot;
     }
 
-    const long long sum_row = (long long)bq * WQ + wq;
+    const long long sum_row = (long long)bq * WQ + wq, top_at = ((long long)bq * tiles_p + bp) * NW + wave;
     if constexpr (EP == EP_STORE) {
-        finish_tile<E, EP, ACT_NONE, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split);
+        finish_tile<E, EP, ACT_NONE, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, top_at, lane, split);
     } else {
         switch (e.act) {                                   // uniform
             case ACT_NONE:
-                if constexpr (EP != EP_DLINEAR) finish_tile<E, EP, ACT_NONE, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split);
+                if constexpr (EP != EP_DLINEAR) finish_tile<E, EP, ACT_NONE, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, top_at, lane, split);
                 break;                                     // (dz is dy as it stands)
-            case ACT_SILU: finish_tile<E, EP, ACT_SILU, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split); break;
-            case ACT_GELU: finish_tile<E, EP, ACT_GELU, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split); break;
-            default: finish_tile<E, EP, ACT_GELU_TANH, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, lane, split); break;
+            case ACT_SILU: finish_tile<E, EP, ACT_SILU, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, top_at, lane, split); break;
+            case ACT_GELU: finish_tile<E, EP, ACT_GELU, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, top_at, lane, split); break;
+            default: finish_tile<E, EP, ACT_GELU_TANH, FP, FQ, WP, WQ>(g, e, acc, n0, m0, wp, wq, sum_row, top_at, lane, split); break;
         }
     }
 }
@@ -433,6 +445,7 @@ __global__ void __launch_bounds__(WP * WQ * 64) gemm_tile_kernel(Operand P, Oper
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int logical = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if (logical >= total) return;                          // uniform per workgroup, before any barrier
+    if ((EP == EP_DLINEAR || EP == EP_DGLU) && store_factor<E, true>(e) == 0.f) return;
     gemm_tile<E, EP, PA, QA, BP, BQ, WP, WQ, NST>(P, Q, g, e, tiles_p, tiles_q, nsplit, logical, lds);
 }
 
@@ -459,14 +472,14 @@ __global__ void __launch_bounds__(WP * WQ * 64) gemm_pair_kernel(PairPart a, Pai
 }
 
 template <typename E, int EP, bool PA, bool QA, int BP, int BQ, int WP, int WQ, int NST>
-hipError_t launch_cfg(const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s, int* sum_rows) {
+hipError_t launch_cfg(const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s, Filled* filled) {
     constexpr bool GLU = EP == EP_GLU || EP == EP_DGLU;
     constexpr int bn = GLU ? BP / 2 : BP, bytes = (BP + BQ) * 128 * NST;
     static_assert(bytes <= 160 * 1024, "LDS budget");
     const long long tp = (g.N + bn - 1) / bn, tq = ((long long)g.M + BQ - 1) / BQ, total = tp * tq * nsplit;
     if (total > 0x3fffffffLL) return hipErrorInvalidValue;
     const int per_xcd = (int)((total + 7) / 8);
-    if (sum_rows) *sum_rows = (int)tq * WQ;
+    if (filled) *filled = Filled{(int)tq * WQ, tp * tq * (WP * WQ)};
     auto kern = gemm_tile_kernel<E, EP, PA, QA, BP, BQ, WP, WQ, NST>;
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (attr != hipSuccess) return attr;
@@ -478,41 +491,41 @@ hipError_t launch_cfg(const Operand& P, const Operand& Q, const GemmShape& g, co
 // 256x256 116 / 41 / 56 / 104, 128x128 with two stages 129 / 34 / 30 / 55, with three 160 / 40 / 23 / 42, 64x64 - / 46 / 26 / 23.  A large block
 // moves the fewest bytes through LDS per flop, but has to fill the chip, and with one workgroup per compute unit its epilogue overlaps with nothing:
 // worth it for long reductions only.  128x128 runs two workgroups per unit where there are enough; where there is about one, a third stage pays.
-template <typename E, int EP, bool PA, bool QA> hipError_t launch_shape(const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s, int* sum_rows) {
+template <typename E, int EP, bool PA, bool QA> hipError_t launch_shape(const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s, Filled* filled) {
     constexpr bool GLU = EP == EP_GLU || EP == EP_DGLU;
     const long long width = GLU ? 2LL * g.N : g.N, t256 = ((width + 255) / 256) * ((g.M + 255) / 256) * nsplit, t128 = ((width + 127) / 128) * ((g.M + 127) / 128) * nsplit;
     const int depth = g.K / nsplit;
     if constexpr (sizeof(E) == 4) {
         // bound by its MFMAs: the large block only where its tiles fill the units evenly (4096^3 144 TFLOP/s of the library's 151)
-        if (t128 >= 768) return launch_cfg<E, EP, PA, QA, 128, 128, 2, 2, 2>(P, Q, g, e, nsplit, s, sum_rows);
-        if constexpr (GLU) return launch_cfg<E, EP, PA, QA, 128, 64, 2, 2, 2>(P, Q, g, e, nsplit, s, sum_rows);
-        else if (depth < 512) return launch_cfg<E, EP, PA, QA, 64, 64, 2, 2, 2>(P, Q, g, e, nsplit, s, sum_rows);
-        else return launch_cfg<E, EP, PA, QA, 64, 64, 2, 2, 3>(P, Q, g, e, nsplit, s, sum_rows);
+        if (t128 >= 768) return launch_cfg<E, EP, PA, QA, 128, 128, 2, 2, 2>(P, Q, g, e, nsplit, s, filled);
+        if constexpr (GLU) return launch_cfg<E, EP, PA, QA, 128, 64, 2, 2, 2>(P, Q, g, e, nsplit, s, filled);
+        else if (depth < 512) return launch_cfg<E, EP, PA, QA, 64, 64, 2, 2, 2>(P, Q, g, e, nsplit, s, filled);
+        else return launch_cfg<E, EP, PA, QA, 64, 64, 2, 2, 3>(P, Q, g, e, nsplit, s, filled);
     } else {
-    if (depth >= 1536 && t256 >= 224) return launch_cfg<E, EP, PA, QA, 256, 256, 2, 4, 2>(P, Q, g, e, nsplit, s, sum_rows);
-    if (t128 >= 320) return launch_cfg<E, EP, PA, QA, 128, 128, 2, 4, 2>(P, Q, g, e, nsplit, s, sum_rows);
-    if (t128 >= 130 && depth >= 1024) return launch_cfg<E, EP, PA, QA, 128, 128, 2, 4, 3>(P, Q, g, e, nsplit, s, sum_rows);
-    if constexpr (GLU) return launch_cfg<E, EP, PA, QA, 128, 64, 2, 2, 3>(P, Q, g, e, nsplit, s, sum_rows);       // u and g in one wave: 64 rows of P each
-    else return launch_cfg<E, EP, PA, QA, 64, 64, 2, 2, 3>(P, Q, g, e, nsplit, s, sum_rows);
+    if (depth >= 1536 && t256 >= 224) return launch_cfg<E, EP, PA, QA, 256, 256, 2, 4, 2>(P, Q, g, e, nsplit, s, filled);
+    if (t128 >= 320) return launch_cfg<E, EP, PA, QA, 128, 128, 2, 4, 2>(P, Q, g, e, nsplit, s, filled);
+    if (t128 >= 130 && depth >= 1024) return launch_cfg<E, EP, PA, QA, 128, 128, 2, 4, 3>(P, Q, g, e, nsplit, s, filled);
+    if constexpr (GLU) return launch_cfg<E, EP, PA, QA, 128, 64, 2, 2, 3>(P, Q, g, e, nsplit, s, filled);       // u and g in one wave: 64 rows of P each
+    else return launch_cfg<E, EP, PA, QA, 64, 64, 2, 2, 3>(P, Q, g, e, nsplit, s, filled);
     }
 }
 
-template <typename E, int EP> hipError_t launch_layout(bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s, int* sum_rows) {
+template <typename E, int EP> hipError_t launch_layout(bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s, Filled* filled) {
     if constexpr (EP == EP_STORE) {
-        if (pa && qa) return launch_shape<E, EP, true, true>(P, Q, g, e, nsplit, s, sum_rows);
-        if (pa) return launch_shape<E, EP, true, false>(P, Q, g, e, nsplit, s, sum_rows);
+        if (pa && qa) return launch_shape<E, EP, true, true>(P, Q, g, e, nsplit, s, filled);
+        if (pa) return launch_shape<E, EP, true, false>(P, Q, g, e, nsplit, s, filled);
     }
-    return launch_shape<E, EP, false, false>(P, Q, g, e, nsplit, s, sum_rows);
+    return launch_shape<E, EP, false, false>(P, Q, g, e, nsplit, s, filled);
 }
 
-template <typename E> hipError_t launch_ep(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s, int* sum_rows) {
+template <typename E> hipError_t launch_ep(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, hipStream_t s, Filled* filled) {
     switch (ep) {
         case EP_STORE:
-        case EP_PART: return launch_layout<E, EP_STORE>(pa, qa, P, Q, g, e, nsplit, s, sum_rows);      // (told apart by e.part)
-        case EP_LINEAR: return launch_layout<E, EP_LINEAR>(pa, qa, P, Q, g, e, nsplit, s, sum_rows);
-        case EP_DLINEAR: return launch_layout<E, EP_DLINEAR>(pa, qa, P, Q, g, e, nsplit, s, sum_rows);
-        case EP_GLU: return launch_layout<E, EP_GLU>(pa, qa, P, Q, g, e, nsplit, s, sum_rows);
-        case EP_DGLU: return launch_layout<E, EP_DGLU>(pa, qa, P, Q, g, e, nsplit, s, sum_rows);
+        case EP_PART: return launch_layout<E, EP_STORE>(pa, qa, P, Q, g, e, nsplit, s, filled);      // (told apart by e.part)
+        case EP_LINEAR: return launch_layout<E, EP_LINEAR>(pa, qa, P, Q, g, e, nsplit, s, filled);
+        case EP_DLINEAR: return launch_layout<E, EP_DLINEAR>(pa, qa, P, Q, g, e, nsplit, s, filled);
+        case EP_GLU: return launch_layout<E, EP_GLU>(pa, qa, P, Q, g, e, nsplit, s, filled);
+        case EP_DGLU: return launch_layout<E, EP_DGLU>(pa, qa, P, Q, g, e, nsplit, s, filled);
         default: return hipErrorInvalidValue;
     }
 }
@@ -564,8 +577,8 @@ bool tile_gemm_ok(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, 
     return (bits & 15) == 0;
 }
 
-hipError_t launch_tile_gemm(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, int dt, hipStream_t s, int* sum_rows) {
-    return with_dtype(dt, [&](auto* tag) -> hipError_t { return launch_ep<std::remove_pointer_t<decltype(tag)>>(ep, pa, qa, P, Q, g, e, nsplit, s, sum_rows); });
+hipError_t launch_tile_gemm(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, int dt, hipStream_t s, Filled* filled) {
+    return with_dtype(dt, [&](auto* tag) -> hipError_t { return launch_ep<std::remove_pointer_t<decltype(tag)>>(ep, pa, qa, P, Q, g, e, nsplit, s, filled); });
 }
 
 }  // namespace wino

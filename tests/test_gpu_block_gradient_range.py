@@ -95,3 +95,76 @@ def test_zero_and_infinite_gradients():
     assert not torch.isfinite(bad["dq"][1, 3]).any() and not torch.isfinite(bad["dk"][1]).any() and not torch.isfinite(bad["dv"][1]).any()
     bad["dq"][1, 3] = clean["dq"][1, 3]
     assert torch.equal(bad["dq"], clean["dq"]) and all(torch.equal(bad[n][0], clean[n][0]) for n in ("dk", "dv"))
+
+
+# ---- products ---------------------------------------------------------------------------------------------------------------------------
+def _product_inputs(M, K, N, halves, std, some):
+    """u and g of unit size, dx and dw of one size; a part `some` of the incoming gradient is not zero, so that sums of a large one stay in range."""
+    W = (M / (halves * N * K)) ** 0.25
+    x, w, b = _rand((M, K), 1, 1 / (W * K ** 0.5)), _rand((halves * N, K), 2, W), torch.randn(halves * N, generator=torch.Generator().manual_seed(3)) * 0.3
+    on = torch.rand((M, N), generator=torch.Generator().manual_seed(5)) < some
+    return x, w, b, torch.where(on, _rand((M, N), 4, std), torch.zeros((), dtype=F16))
+
+
+def _product_gradients(glu, x, w, b, dy, act="gelu"):
+    code = {"silu": B.WINO_ACT_SILU, "gelu": B.WINO_ACT_GELU, "gelu_tanh": B.WINO_ACT_GELU_TANH, "none": B.WINO_ACT_NONE}[act]
+    got = (B.glu_backward if glu else B.linear_backward)(*(t.to(DEV) for t in (x, w, b, dy)), code)
+    want = (O.glu_backward if glu else O.linear_backward)(x.double(), w.double(), b.double(), dy.double(), act, F16)
+    return [(n, g, r) for n, g, (r, _) in zip(("dx", "dw", "dbias"), got, want)]
+
+
+# every kernel that stores or takes the gradients of the pre-activations: blocks of 128 and 64, any alignment, ranges with their join, few rows
+@pytest.mark.parametrize("M,K,N", [(16, 256, 128), (40, 77, 33), (300, 200, 136), (700, 640, 200), (90, 1032, 320), (1500, 515, 333), (2100, 328, 640)])
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("std", [2.0 ** -18, 2.0 ** -13, 1.0, 2.0 ** 11])
+def test_gradients_of_products_at_any_size_of_the_incoming_one(M, K, N, glu, std):
+    x, w, b, dy = _product_inputs(M, K, N, 2 if glu else 1, std, 0.1 if std > 1 else 1.0)
+    for act in ("gelu", "silu"):
+        for n, g, r in _product_gradients(glu, x, w, b, dy, act):
+            if n == "dbias":
+                assert ((g.cpu().double() - r).norm() / r.norm()).item() < 1e-5, (act, n)
+            else:
+                _two_roundings(g, r, (act, n))
+
+
+def test_gradients_of_preactivations_beyond_the_range():
+    """du and dg pass 65504, the gradients of x and w do not; one result alone, and from a strided gradient."""
+    M, K, N = 700, 2000, 136
+    x, w, b, dy = _product_inputs(M, K, N, 2, 2.0 ** 13, 0.1)
+    z = x.double() @ w.double().T + b.double()
+    u, g = z[:, :N], z[:, N:]
+    slope = torch.special.ndtr(g) + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+    assert (dy.double() * u * slope).abs().max() > 65504
+    (_, dx, rx), (_, dw, rw), _ = _product_gradients(True, x, w, b, dy)
+    _two_roundings(dx, rx, "dx")
+    _two_roundings(dw, rw, "dw")
+    ws = torch.full((B.wino_glu_backward_workspace_bytes(M, N, K, B.WINO_F16, B.WINO_ACT_GELU),), 255, dtype=torch.uint8, device=DEV)
+    wide = torch.full((M, N + 8), math.nan, dtype=F16, device=DEV)
+    wide[:, :N] = dy.to(DEV)
+    for which in (0, 1):
+        out = [torch.empty_like(t.to(DEV)) for t in (x, w)]
+        B.wino_glu_backward(x.to(DEV), w.to(DEV), b.to(DEV), wide[:, :N], out[0] if which == 0 else None, out[1] if which == 1 else None, None, workspace=ws)
+        assert torch.equal(out[which], (dx, dw)[which])
+
+
+def test_replays_follow_the_size_of_the_gradient():
+    """Whether the gradients of the pre-activations are formed again is decided on the GPU: one captured call, gradients of several sizes."""
+    M, K, N = 300, 200, 136
+    x, w, b, dy = (t.to(DEV) for t in _product_inputs(M, K, N, 2, 1.0, 0.05))
+    sizes = [dy, dy * 2.0 ** 12, dy * 2.0 ** -15, torch.zeros_like(dy)]
+    want = [B.glu_backward(x, w, b, t) for t in sizes]
+    out = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+    ws = torch.empty(B.wino_glu_backward_workspace_bytes(M, N, K, B.WINO_F16, B.WINO_ACT_GELU), dtype=torch.uint8, device=DEV)
+    given = dy.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        B.wino_glu_backward(x, w, b, given, *out, workspace=ws)
+    for n in (0, 1, 2, 1, 3, 0):
+        given.copy_(sizes[n])
+        for o in out:
+            o.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, r) for o, r in zip(out, want[n])), n
+        B.glu_backward(x, w, b, dy)
