@@ -373,8 +373,9 @@ int wino_i8_batched_gemm(const void *Uq, const float *dU, const void *Vq, const 
  * [du | dg] below).  That, and the softmax weights and their gradients inside the attention kernels, are operands of the next matrix
  * product and are rounded to `dtype` for it.  (fp16: the gradients of the pre-activations times a power of two of the call where their
  * largest finite one is below 1 or beyond 65504, those of the softmax scores times one of each query row or key, so that only what the
- * results themselves cannot hold is lost to the type's range.)  Attention and, with two-byte types, the activations take the hardware's exponential
- * and reciprocal (one unit in the last place of fp32); the activations of fp32 calls take the library's functions.
+ * results themselves cannot hold is lost to the type's range.)  Attention takes the hardware's exponential (one unit in the last place
+ * of fp32).  The activations of two-byte calls take the hardware's exponential and reciprocal, and GELU with erf a formula whose value is off
+ * by at most 1e-4 of itself; those of fp32 calls take the library's functions.
  * "Overlap" is taken from the first to the last byte of a tensor, gaps between strided rows included.
  * A workspace belongs to one call at a time: calls on different streams, and graphs that may run at the same time, need one each.
  * Sizes with no effect on it may be anything; the *_workspace_bytes calls return 0 where none is needed (then workspace may be NULL)

@@ -10,7 +10,7 @@ import torch
 UNIT = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
 FLOOR = {torch.float32: 0.0, torch.float16: 2.0 ** -25, torch.bfloat16: 0.0}
 F32 = 2.0 ** -24
-# The activations in fp32: distribution functions within 3e-7 (the series for erf 1.5e-7, exponential and reciprocal one unit each), times |z|;
+# The activations in fp32: distribution functions within 3e-7 (GELU's formula 1e-7, exponential and reciprocal one unit each), times |z|;
 # the derivative adds |z| c'(z), of the same kind.
 ACT_ERROR = 4e-7
 
@@ -23,10 +23,10 @@ def act(z, kind):
         c = 1 / (1 + torch.exp(-z))
         return z * c, c + z * c * (1 - c)
     if kind == "gelu":
-        c = torch.special.ndtr(z)
+        c = torch.special.erfc(-z * math.sqrt(0.5)) / 2                  # (small values too are right relative to themselves)
         return z * c, c + z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
-    t = torch.tanh(math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3))
-    return z * (1 + t) / 2, (1 + t) / 2 + z / 2 * (1 - t * t) * math.sqrt(2 / math.pi) * (1 + 3 * 0.044715 * z * z)
+    c = torch.sigmoid(2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3))       # (1 + tanh t) / 2
+    return z * c, c + 2 * z * c * (1 - c) * math.sqrt(2 / math.pi) * (1 + 3 * 0.044715 * z * z)
 
 
 def _rounded(v, dtype):
