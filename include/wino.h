@@ -429,8 +429,8 @@ int wino_glu_backward(const void *x, const void *w, const float *bias, const voi
  *   lse[b][h][i] = log sum_j exp(s_ij), fp32 [B][H][Sq]; NULL where no backward pass follows.
  * Tensors are [batch][position][head][D] with strides of their own in elements (a slice of a packed q,k,v product is read in place);
  * D is contiguous, a multiple of 8, at most 256 (fp32: 160).  Strides are not negative and multiples of 16 bytes; those of outputs
- * are positive, and each spans what the smaller ones reach, so that no two positions meet (WINO_ERR_DIM).  scale > 0.  Outputs must
- * not overlap inputs.  Gradients may share a packed buffer where they have the same strides and none of their positions meet.
+ * are positive, and each spans what the smaller ones reach, so that no two positions meet (WINO_ERR_DIM).  scale > 0.  Outputs (the
+ * forward call's lse among them) must not overlap inputs or each other.  Gradients may share a packed buffer where they have the same strides and none of their positions meet.
  * H * Sq, B * H * Sq, Skv and B * Hkv * Skv are at most 2^29, B * Hkv at most 2^22.
  */
 typedef struct wino_tensor { void *data; long long stride_b, stride_s, stride_h; } wino_tensor;

@@ -241,6 +241,11 @@ int attention_status(const wino_attention_args* a, bool backward) {
             overlap(p, np, a->key_mask, (size_t)a->B * a->Skv))
             return WINO_ERR_ALIAS;
     }
+    if (!backward && a->lse) {                             // an output there
+        const size_t n_lse = (size_t)a->B * a->H * a->Sq * 4;
+        for (int i = 0; i < 3; ++i) if (overlap(a->lse, n_lse, items[i].t->data, size(items[i]))) return WINO_ERR_ALIAS;
+        if (overlap(a->lse, n_lse, a->kv_len, (size_t)a->B * 4) || overlap(a->lse, n_lse, a->key_mask, (size_t)a->B * a->Skv)) return WINO_ERR_ALIAS;
+    }
     return WINO_OK;
 }
 
