@@ -377,7 +377,8 @@ int wino_i8_batched_gemm(const void *Uq, const float *dU, const void *Vq, const 
  * of fp32).  The activations of two-byte calls take the hardware's exponential and reciprocal, and GELU with erf a formula whose value is off
  * by at most 1e-4 of itself; those of fp32 calls take the library's functions.
  * "Overlap" is taken from the first to the last byte of a tensor, gaps between strided rows included.
- * A workspace belongs to one call at a time: calls on different streams, and graphs that may run at the same time, need one each.
+ * A workspace (as many bytes of it as the call needs) must not overlap any tensor of the call (WINO_ERR_ALIAS).
+ * It belongs to one call at a time: calls on different streams, and graphs that may run at the same time, need one each.
  * Sizes with no effect on it may be anything; the *_workspace_bytes calls return 0 where none is needed (then workspace may be NULL)
  * and for bad arguments.
  */
@@ -430,7 +431,8 @@ int wino_glu_backward(const void *x, const void *w, const float *bias, const voi
  * Tensors are [batch][position][head][D] with strides of their own in elements (a slice of a packed q,k,v product is read in place);
  * D is contiguous, a multiple of 8, at most 256 (fp32: 160).  Strides are not negative and multiples of 16 bytes; those of outputs
  * are positive, and each spans what the smaller ones reach, so that no two positions meet (WINO_ERR_DIM).  scale > 0.  Outputs (the
- * forward call's lse among them) must not overlap inputs or each other.  Gradients may share a packed buffer where they have the same strides and none of their positions meet.
+ * forward call's lse among them) must not overlap inputs or each other, except that gradients may share a packed buffer where they have
+ * the same strides and none of their positions meet.
  * H * Sq, B * H * Sq, Skv and B * Hkv * Skv are at most 2^29, B * Hkv at most 2^22.
  */
 typedef struct wino_tensor { void *data; long long stride_b, stride_s, stride_h; } wino_tensor;

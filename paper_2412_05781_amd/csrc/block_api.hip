@@ -98,6 +98,8 @@ int products_backward(const void* x, const void* w, const float* bias, const voi
     BackwardSpace b = backward_space(M, W, K, dt, stored, halves);
     if (!workspace || workspace_bytes < b.total) return WINO_ERR_WORKSPACE;
     if (!at16(workspace)) return WINO_ERR_ALIGN;
+    for (const auto& t : in) if (overlap(workspace, b.total, t.p, t.n)) return WINO_ERR_ALIAS;
+    for (const auto& t : out) if (overlap(workspace, b.total, t.p, t.n)) return WINO_ERR_ALIAS;
     hipStream_t s = static_cast<hipStream_t>(stream);
     unsigned char* base = static_cast<unsigned char*>(workspace);
     float* sums = reinterpret_cast<float*>(base + b.dz);
@@ -198,7 +200,7 @@ bool gradients_meet(const wino_tensor& x, const int (&nx)[3], const wino_tensor&
 
 AttnTensor inner(const wino_tensor& t) { return AttnTensor{t.data, t.stride_b, t.stride_s, t.stride_h}; }
 
-int attention_status(const wino_attention_args* a, bool backward) {
+int attention_status(const wino_attention_args* a, bool backward, const void* workspace, size_t workspace_bytes) {
     if (!a) return WINO_ERR_NULL;
     if (!is_dtype(a->dtype)) return WINO_ERR_DTYPE;
     if (!attention_dims_ok(a->B, a->Sq, a->Skv, a->H, a->Hkv, a->D, a->dtype) || !(a->scale > 0.f) || !isfinite(a->scale)) return WINO_ERR_DIM;
@@ -246,6 +248,14 @@ int attention_status(const wino_attention_args* a, bool backward) {
         for (int i = 0; i < 3; ++i) if (overlap(a->lse, n_lse, items[i].t->data, size(items[i]))) return WINO_ERR_ALIAS;
         if (overlap(a->lse, n_lse, a->kv_len, (size_t)a->B * 4) || overlap(a->lse, n_lse, a->key_mask, (size_t)a->B * a->Skv)) return WINO_ERR_ALIAS;
     }
+    const size_t need = backward ? attention_backward_ws_bytes(a->B, a->Sq, a->Skv, a->H, a->Hkv, a->D, a->dtype) : attention_ws_bytes(a->B, a->Sq, a->Skv, a->H, a->Hkv, a->D, a->dtype);
+    if (!need) return WINO_OK;
+    if (!workspace || workspace_bytes < need) return WINO_ERR_WORKSPACE;
+    if (!at16(workspace)) return WINO_ERR_ALIGN;
+    for (int i = 0; i < n; ++i) if (overlap(workspace, need, items[i].t->data, size(items[i]))) return WINO_ERR_ALIAS;
+    if (overlap(workspace, need, a->lse, (size_t)a->B * a->H * a->Sq * 4) || overlap(workspace, need, a->kv_len, (size_t)a->B * 4) ||
+        overlap(workspace, need, a->key_mask, (size_t)a->B * a->Skv))
+        return WINO_ERR_ALIAS;
     return WINO_OK;
 }
 
@@ -280,7 +290,12 @@ int wino_linear(const void* x, const void* w, const float* bias, const void* res
     if (residual && !(residual == y && ldr == ldy) && overlap(y, ny, residual, extent(M, ldr, N, es))) return WINO_ERR_ALIAS;
     const size_t need = few_gemm_ok(M) ? 0 : product_bytes(M, N, K, dtype);
     if (need && (!workspace || workspace_bytes < need)) return WINO_ERR_WORKSPACE;
-    if (need && !at16(workspace)) return WINO_ERR_ALIGN;
+    if (need) {
+        if (!at16(workspace)) return WINO_ERR_ALIGN;
+        if (overlap(workspace, need, y, ny) || overlap(workspace, need, x, extent(M, ldx, K, es)) || overlap(workspace, need, w, (size_t)N * K * es) ||
+            overlap(workspace, need, bias, (size_t)N * 4) || overlap(workspace, need, residual, extent(M, ldr, N, es)))
+            return WINO_ERR_ALIAS;
+    }
     Epilogue e;
     e.bias = bias; e.extra = residual; e.ld_extra = ldr; e.out = y; e.ld_out = ldy; e.act = act;
     const Operand P{w, K}, Q{x, ldx};
@@ -337,11 +352,8 @@ size_t wino_attention_workspace_bytes(int B, int Sq, int Skv, int H, int Hkv, in
 }
 
 int wino_attention(const wino_attention_args* a, void* workspace, size_t workspace_bytes, void* stream) {
-    const int rc = attention_status(a, false);
+    const int rc = attention_status(a, false, workspace, workspace_bytes);
     if (rc != WINO_OK) return rc;
-    const size_t need = attention_ws_bytes(a->B, a->Sq, a->Skv, a->H, a->Hkv, a->D, a->dtype);
-    if (need && (!workspace || workspace_bytes < need)) return WINO_ERR_WORKSPACE;
-    if (need && !at16(workspace)) return WINO_ERR_ALIGN;
     return launch_attention(attention_args(a, workspace), a->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? WINO_OK : WINO_ERR_HIP;
 }
 
@@ -351,11 +363,8 @@ size_t wino_attention_backward_workspace_bytes(int B, int Sq, int Skv, int H, in
 }
 
 int wino_attention_backward(const wino_attention_args* a, void* workspace, size_t workspace_bytes, void* stream) {
-    const int rc = attention_status(a, true);
+    const int rc = attention_status(a, true, workspace, workspace_bytes);
     if (rc != WINO_OK) return rc;
-    const size_t need = attention_backward_ws_bytes(a->B, a->Sq, a->Skv, a->H, a->Hkv, a->D, a->dtype);
-    if (!workspace || workspace_bytes < need) return WINO_ERR_WORKSPACE;
-    if (!at16(workspace)) return WINO_ERR_ALIGN;
     return launch_attention_backward(attention_args(a, workspace), a->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? WINO_OK : WINO_ERR_HIP;
 }
 

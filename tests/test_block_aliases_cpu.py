@@ -52,3 +52,39 @@ def test_lse_is_an_input_of_the_backward_call(L):
     assert _call(L, True) == B.WINO_ERR_WORKSPACE and _call(L, False, lse=None) == B.WINO_ERR_WORKSPACE
     for at in (DQ, DK, DV):
         assert _call(L, True, lse=at) == B.WINO_ERR_ALIAS
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_workspace_of_attention_overlaps_nothing(L, backward):
+    need = _need(backward)
+    tensors = [(Q, BYTES["q"]), (K, BYTES["k"]), (V, BYTES["v"]), (O, BYTES["o"]), (LSE, LSE_BYTES), (LENS, 8), (MASK, 18000)]
+    if backward:
+        tensors += [(DO, BYTES["q"]), (DQ, BYTES["q"]), (DK, BYTES["k"]), (DV, BYTES["v"])]
+    for at, size in tensors:
+        for ws in (at, at + (size - 1) // 16 * 16, at - (need - 1) // 16 * 16):
+            assert _call(L, backward, ws=ws, n=need) == B.WINO_ERR_ALIAS, (hex(at), hex(ws))
+            assert _call(L, backward, ws=ws, n=1 << 40) == B.WINO_ERR_ALIAS, (hex(at), hex(ws))
+
+
+X, W, BIAS, R, Y, DX, DW, DB = (SPACE * i for i in range(21, 29))
+M, N, KK = 80, 64, 4096
+
+
+def test_workspace_of_products_overlaps_nothing(L):
+    need = B.wino_linear_workspace_bytes(M, N, KK, B.WINO_F16)
+    assert need > 0
+    call = lambda ws: L.wino_linear(X, W, BIAS, R, Y, M, N, KK, KK, N, N, B.WINO_F16, 0, ws, need, None)
+    for at, size in ((X, M * KK * 2), (W, N * KK * 2), (BIAS, N * 4), (R, M * N * 2), (Y, M * N * 2)):
+        for ws in (at, at + size - 16, at - (need - 1) // 16 * 16):
+            assert call(ws) == B.WINO_ERR_ALIAS, (hex(at), hex(ws))
+
+
+@pytest.mark.parametrize("which,halves", [("wino_linear_backward", 1), ("wino_glu_backward", 2)])
+@pytest.mark.parametrize("act", [0, 2])
+def test_workspace_of_product_gradients_overlaps_nothing(L, which, halves, act):
+    need = getattr(B, which + "_workspace_bytes")(M, N, KK, B.WINO_F16, act)
+    call = lambda ws: getattr(L, which)(X, W, BIAS, Y, DX, DW, DB, M, N, KK, KK, N, KK, B.WINO_F16, act, ws, need, None)
+    w = halves * N
+    for at, size in ((X, M * KK * 2), (W, w * KK * 2), (BIAS, w * 4), (Y, M * N * 2), (DX, M * KK * 2), (DW, w * KK * 2), (DB, w * 4)):
+        for ws in (at, at + size - 16, at - (need - 1) // 16 * 16):
+            assert call(ws) == B.WINO_ERR_ALIAS, (hex(at), hex(ws))
