@@ -812,10 +812,11 @@ def _scratch(nbytes, like):
 
 
 def _flat(t):
-    """t as rows of its last dimension, copied where the rows are not contiguous (an expanded gradient, a transposed tensor)."""
+    """t as rows of its last dimension, copied where the rows are not contiguous (an expanded gradient, a transposed tensor) or do not start at a multiple of 16 bytes."""
     t = t.reshape(-1, t.shape[-1])
     ld, step = t.stride()
-    return t if (step == 1 or t.shape[1] == 1) and (ld >= t.shape[1] or t.shape[0] == 1) else t.contiguous()
+    fits = (step == 1 or t.shape[1] == 1) and (ld >= t.shape[1] or t.shape[0] == 1) and t.data_ptr() % 16 == 0
+    return t if fits else t.clone(memory_format=torch.contiguous_format)
 
 
 def _packed(t):
