@@ -811,6 +811,12 @@ def _scratch(nbytes, like):
     return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
 
 
+def _no_history(name, *tensors):
+    """These calls record nothing for autograd, and refuse tensors whose gradients would get lost that way."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError(f"{name} records no history: call it under torch.no_grad() or on detached tensors, and {name}_backward for the gradients")
+
+
 def _flat(t):
     """t as rows of its last dimension, copied where the rows are not contiguous (an expanded gradient, a transposed tensor) or do not start at a multiple of 16 bytes."""
     t = t.reshape(-1, t.shape[-1])
@@ -827,6 +833,7 @@ def _packed(t):
 
 def linear(x, w, bias=None, act: int = WINO_ACT_NONE, residual=None):
     """act(x w^T + bias) + residual over the last dimension of x, with the output and the workspace allocated here."""
+    _no_history("linear", x, w, bias, residual)
     x2, N = _flat(x), int(w.shape[0])
     y = torch.empty((x2.shape[0], N), dtype=x.dtype, device=x.device)
     ws = _scratch(wino_linear_workspace_bytes(x2.shape[0], N, x2.shape[1], DTYPE_OF[x.dtype], act), x)
@@ -845,6 +852,7 @@ def linear_backward(x, w, bias, dy, act: int = WINO_ACT_NONE):
 
 def glu(x, w, bias=None, act: int = WINO_ACT_GELU):
     """(x wu^T + bu) * act(x wg^T + bg) over the last dimension of x."""
+    _no_history("glu", x, w, bias)
     x2, N = _flat(x), int(w.shape[0]) // 2
     h = torch.empty((x2.shape[0], N), dtype=x.dtype, device=x.device)
     ws = _scratch(wino_glu_workspace_bytes(x2.shape[0], N, x2.shape[1], DTYPE_OF[x.dtype], act), x)
@@ -863,6 +871,7 @@ def glu_backward(x, w, bias, dh, act: int = WINO_ACT_GELU):
 
 def attention(q, k, v, kv_len=None, key_mask=None, scale=None, with_lse: bool = False):
     """softmax(scale q k^T) v; with_lse: (o, lse), what attention_backward takes."""
+    _no_history("attention", q, k, v)
     q, k, v = _packed(q), _packed(k), _packed(v)
     (B, Sq, H, D), (_, Skv, Hkv, _) = q.shape, k.shape
     o = torch.empty((B, Sq, H, D), dtype=q.dtype, device=q.device)

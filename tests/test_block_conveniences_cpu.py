@@ -13,3 +13,21 @@ def test_rows_that_start_off_a_boundary_are_copied():
         f = B._flat(t)
         assert f.data_ptr() % 16 == 0 and torch.equal(f, t.reshape(-1, t.shape[-1])) and f.stride(1) == 1
     assert B._flat(x[:, :70]).data_ptr() == x.data_ptr()               # at a boundary: where it is
+
+
+def test_tensors_that_need_a_gradient_are_refused():
+    """These calls record no history: a result without one would end a training step's gradients in silence."""
+    x, w, b = torch.zeros(4, 16), torch.zeros(8, 16), torch.zeros(8)
+    q, k = torch.zeros(1, 3, 2, 16), torch.zeros(1, 5, 2, 16)
+    leaf = lambda t: t.clone().requires_grad_()
+    calls = [lambda: B.linear(leaf(x), w, b), lambda: B.linear(x, leaf(w), b), lambda: B.linear(x, w, leaf(b)), lambda: B.linear(x, w, b, residual=leaf(torch.zeros(4, 8))),
+             lambda: B.glu(leaf(x), w, b), lambda: B.glu(x, leaf(w), b), lambda: B.glu(x, w, leaf(b)), lambda: B.linear(leaf(x) * 2, w, b),
+             lambda: B.attention(leaf(q), k, k), lambda: B.attention(q, leaf(k), k), lambda: B.attention(q, k, leaf(k), with_lse=True)]
+    for call in calls:
+        with pytest.raises(ValueError, match="_backward"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU"):                       # goes on to the next check
+            call()
+    for call in (lambda: B.linear(leaf(x).detach(), w, b), lambda: B.linear_backward(x, leaf(w), b, torch.zeros(4, 8))):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
