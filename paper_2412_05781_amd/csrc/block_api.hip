@@ -275,7 +275,7 @@ extern "C" {
 
 size_t wino_linear_workspace_bytes(int M, int N, int K, int dtype, int act) {
     if (!is_dtype(dtype) || !is_act(act) || !product_dims_ok(M, N, K, 1)) return 0;
-    return few_gemm_ok(M) ? 0 : product_bytes(M, N, K, dtype);
+    return few_gemm_ok(false, M, N, K, dtype, true) ? 0 : product_bytes(M, N, K, dtype);
 }
 
 int wino_linear(const void* x, const void* w, const float* bias, const void* residual, void* y, int M, int N, int K, long long ldx, long long ldr,
@@ -288,7 +288,12 @@ int wino_linear(const void* x, const void* w, const float* bias, const void* res
     const size_t es = bytes_of(dtype), ny = extent(M, ldy, N, es);
     if (overlap(y, ny, x, extent(M, ldx, K, es)) || overlap(y, ny, w, (size_t)N * K * es) || overlap(y, ny, bias, (size_t)N * 4)) return WINO_ERR_ALIAS;
     if (residual && !(residual == y && ldr == ldy) && overlap(y, ny, residual, extent(M, ldr, N, es))) return WINO_ERR_ALIAS;
-    const size_t need = few_gemm_ok(M) ? 0 : product_bytes(M, N, K, dtype);
+    Epilogue e;
+    e.bias = bias; e.extra = residual; e.ld_extra = ldr; e.out = y; e.ld_out = ldy; e.act = act;
+    const Operand P{w, K}, Q{x, ldx};
+    const GemmShape g{M, N, K};
+    const bool few = few_gemm_ok(false, M, N, K, dtype, tile_gemm_ok(EP_LINEAR, false, false, P, Q, g, e, dtype));
+    const size_t need = few ? 0 : product_bytes(M, N, K, dtype);
     if (need && (!workspace || workspace_bytes < need)) return WINO_ERR_WORKSPACE;
     if (need) {
         if (!at16(workspace)) return WINO_ERR_ALIGN;
@@ -296,12 +301,8 @@ int wino_linear(const void* x, const void* w, const float* bias, const void* res
             overlap(workspace, need, bias, (size_t)N * 4) || overlap(workspace, need, residual, extent(M, ldr, N, es)))
             return WINO_ERR_ALIAS;
     }
-    Epilogue e;
-    e.bias = bias; e.extra = residual; e.ld_extra = ldr; e.out = y; e.ld_out = ldy; e.act = act;
-    const Operand P{w, K}, Q{x, ldx};
-    const GemmShape g{M, N, K};
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const hipError_t rc = few_gemm_ok(M) ? launch_few_gemm(false, P, Q, g, e, dtype, s) : product(EP_LINEAR, false, false, P, Q, g, e, workspace, dtype, s);
+    const hipError_t rc = few ? launch_few_gemm(false, P, Q, g, e, dtype, s) : product(EP_LINEAR, false, false, P, Q, g, e, workspace, dtype, s);
     return rc == hipSuccess ? WINO_OK : WINO_ERR_HIP;
 }
 
@@ -332,7 +333,7 @@ int wino_glu(const void* x, const void* w, const float* bias, void* h, int M, in
     const Operand P{w, K}, Q{x, ldx};
     const GemmShape g{M, N, K};
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const hipError_t rc = few_gemm_ok(M) ? launch_few_gemm(true, P, Q, g, e, dtype, s) : launch_gemm(EP_GLU, false, false, P, Q, g, e, 1, dtype, s);
+    const hipError_t rc = few_gemm_ok(true, M, N, K, dtype, false) ? launch_few_gemm(true, P, Q, g, e, dtype, s) : launch_gemm(EP_GLU, false, false, P, Q, g, e, 1, dtype, s);
     return rc == hipSuccess ? WINO_OK : WINO_ERR_HIP;
 }
 

@@ -49,6 +49,8 @@ struct GemmShape { int M, N, K; };
 struct Product { Operand P, Q; GemmShape g; Epilogue e; int nsplit; };
 
 bool gemm_dims_ok(long long M, long long N, long long K);
+// whether the kernel for operands that can be fetched 16 bytes at a time (linear_tile.hip) takes a call
+bool tile_gemm_ok(int ep, bool p_trans, bool q_trans, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int dt);
 // rows of Epilogue::sums and number of Epilogue::tops that a launch with EP_DLINEAR / EP_DGLU may fill; launch_gemm says how many it did (may be null)
 int gemm_most_sum_rows(int M);
 long long gemm_most_tops(int M, int N);
@@ -60,8 +62,9 @@ hipError_t launch_gemm(int ep, bool p_trans, bool q_trans, const Operand& P, con
 struct ColumnSums { const void* x; long long ld; int M, N; float* out; int ranges; bool f32; };
 // a = dz w (P across, Q along the reduction) and b = dz^T x (both across), with EP_STORE or ranges; and the column sums c
 hipError_t launch_gemm_pair(const Product& a, const Product& b, const ColumnSums& c, int dt, hipStream_t s);
-// x W^T with EP_LINEAR or (glu) EP_GLU for few rows, one kernel, no workspace
-bool few_gemm_ok(int M);
+// x W^T with EP_LINEAR or (glu) EP_GLU for few rows, one kernel, no workspace.  Whether it is taken; tiles: whether the kernel for aligned operands is the other choice
+// (true never takes it where false does not)
+bool few_gemm_ok(bool glu, int M, int N, int K, int dt, bool tiles);
 hipError_t launch_few_gemm(bool glu, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s);
 // out = act(sum over ranges + bias) + extra
 hipError_t launch_join(const float* part, int nsplit, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s);

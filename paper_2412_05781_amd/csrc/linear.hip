@@ -336,7 +336,9 @@ long long gemm_most_tops(int M, int N) { return 4 * (((long long)M + 63) / 64 + 
 // How many ranges a reduction is cut into: the number with the least time by this count.  A stage of a 64x64 tile takes a workgroup 0.29 us where it waits
 // for its operands (two-byte types, up to 768 workgroups side by side: 512 x 5120 x 1280, 160 tiles, 23 us) and 0.49 us of a compute unit's MFMAs for
 // fp32, where what counts is how evenly the tiles fill the units (2028 x 2560 x 640, 320 tiles: one range 88 us, four 70).  A join is 5 us and the
-// ranges' sums written and read.  Two-byte products with enough tiles of 128x128 are not cut at all.
+// ranges' sums written and read.  Two-byte products with enough tiles of 128x128 are not cut at all.  The ranges together may reach a larger block (launch_shape), which is
+// only faster.  us, one range / as counted / as counted in 64x64 (M x K x N, fp16): 90 x 5120 x 320 22.5 / 9.0 / 9.0, 256 x 2560 x 1280 13.2 / 12.3 / 12.0, 512 x 10240 x 1280
+// 42.6 / 27.8 / 34.8, 1000 x 5120 x 1280 32.0 / 30.2 / 32.8; odd 90 x 2563 x 320 41.6 / 18.7, 1000 x 5123 x 1280 85.8 / 58.9; fp32 2028 x 2560 x 320 52.0 / 38.5.
 int gemm_ranges(int M, int N, int K, int dt) {
     auto tiles = [&](int n, int m) { return (((long long)N + n - 1) / n) * (((long long)M + m - 1) / m); };
     const bool f32 = dt == DT_F32;

@@ -125,7 +125,18 @@ template <typename E, bool GLU> hipError_t launch_rows(const Operand& P, const O
 
 }  // namespace
 
-bool few_gemm_ok(int M) { return M <= 64; }
+// The kernel's time grows with the rows and the reduction, and from 2560 columns on with those; the tiles' hardly does, but they have fewer workgroups, and for the
+// gated product no ranges of the reduction.  us, this kernel / tiles (N x K, fp16): 1 row 320 x 1280 3.9 / 8.9, 1280 x 5120 8.7 / 9.1; 16 rows 640 x 2560 6.9 / 7.8, 1280 x
+// 5120 12.2 / 9.6; 32 rows 1280 x 1280 6.0 / 8.6, 640 x 2560 9.2 / 7.9, 5120 x 1280 10.0 / 9.4; 64 rows 320 x 320 4.5 / 5.1, 1280 x 1280 8.5 / 8.7, 1280 x 5120 25.3 / 11.1;
+// fp32 32 rows 1280 x 1280 9.5 / 11.6, 64 rows 15.1 / 12.0; odd reductions 64 rows 320 x 1283 19.2 / 26.4, 1280 x 5123 67 / 21.5, fp32 32 rows 1280 x 5123 28.7 / 30.0.
+// Gated: 64 rows 1280 x 1280 10.2 / 11.2, 1280 x 5120 30.4 / 33.0, 5120 x 1280 17.6 / 11.9 (17 rows 10.6 / 11.7), fp32 5120 x 1280 40.4 / 49.1.
+bool few_gemm_ok(bool glu, int M, int N, int K, int dt, bool tiles) {
+    if (M > 64) return false;
+    const bool f32 = dt == DT_F32;
+    if (glu) return (long long)M * N <= (f32 ? 400000 : 164000);
+    const double work = (double)M * K * (N > 2560 ? N / 2560. : 1.);
+    return work <= (f32 ? (tiles ? 40960. : 163840.) : (tiles ? 65536. : 82400.));
+}
 
 hipError_t launch_few_gemm(bool glu, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int dt, hipStream_t s) {
     return with_dtype(dt, [&](auto* tag) -> hipError_t {

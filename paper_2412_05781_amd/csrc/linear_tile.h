@@ -126,8 +126,7 @@ template <typename E> inline bool vec_rows(const Operand& o) {
     return ((reinterpret_cast<uintptr_t>(o.p) | (uintptr_t)(o.ld * (long long)sizeof(E))) & 15u) == 0;
 }
 
-// The kernel for operands that can be fetched 16 bytes at a time (linear_tile.hip): whether it takes a call, and the launch.
-bool tile_gemm_ok(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int dt);
+// the launch of a call that tile_gemm_ok lets through
 hipError_t launch_tile_gemm(int ep, bool pa, bool qa, const Operand& P, const Operand& Q, const GemmShape& g, const Epilogue& e, int nsplit, int dt, hipStream_t s, Filled* filled);
 
 // two products in one launch: a with P across and Q along the reduction, b with both across; and the column sums, where c.out is set

@@ -31,3 +31,22 @@ def test_tensors_that_need_a_gradient_are_refused():
     for call in (lambda: B.linear(leaf(x).detach(), w, b), lambda: B.linear_backward(x, leaf(w), b, torch.zeros(4, 8))):
         with pytest.raises(ValueError, match="GPU"):
             call()
+
+
+def test_workspace_of_few_rows_is_never_more_than_asked_for():
+    """A call of few rows may take the kernel without a workspace where the size call, which does not know the strides, counted on the other one; never the reverse."""
+    import os
+    if not os.path.exists(B.LIB_PATH):
+        from paper_2412_05781_amd.build import build_libwino
+        build_libwino()
+    at = [0x100000000 * i for i in range(1, 5)]
+    L = B.lib()
+    for M in (1, 16, 33, 64):
+        for K in (8, 1288, 2563, 5120, 20000):
+            for N in (8, 320, 2568, 10240):
+                for dt in (B.WINO_F16, B.WINO_F32):
+                    need = B.wino_linear_workspace_bytes(M, N, K, dt)
+                    if need:                                  # then aligned operands do need it: a byte less is refused
+                        assert K > 1000
+                        rc = L.wino_linear(at[0], at[1], None, None, at[2], M, N, K, (K + 7) // 8 * 8, N, N, dt, 0, at[3] * 8, need - 1, None)
+                        assert rc == B.WINO_ERR_WORKSPACE or K % 8, (M, K, N, dt)

@@ -109,3 +109,19 @@ def test_each_gradient_alone(M, K, N, dtype, glu):
                 bound = sums[i] + (2 * (O.UNIT[dtype] * whole[i].float().abs() + O.FLOOR[dtype]) if i < 2 else 0)
                 over = ((some[i].float() - whole[i].float()).abs() - 1.02 * bound).max().item()
                 assert over <= 0, (keep, i, act, over)           # (NaN, what was there before, is not)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("M", [1, 9, 16, 17, 40, 64])
+@pytest.mark.parametrize("K,N", [(5120, 1280), (5123, 136), (1288, 5120), (2048, 72)])
+def test_few_rows_and_long_reductions(M, K, N, dtype):
+    """Either side of the rule that leaves few rows to the tiles, with the workspace that the size call asks for and no more."""
+    x, w, b, r = _rand((M, K), dtype, 1), _rand((N, K), dtype, 2, K ** -0.5), _rand((N,), F32, 3), _rand((M, N), dtype, 4)
+    n = B.wino_linear_workspace_bytes(M, N, K, B.DTYPE_OF[dtype], B.WINO_ACT_SILU)
+    out = torch.full((M + 1, N), 7.0, dtype=dtype, device=DEV)
+    B.wino_linear(x.to(DEV), w.to(DEV), b.to(DEV), out[:M], B.WINO_ACT_SILU, r.to(DEV), _space(n) if n else None)
+    ref, bound = O.linear(x.double(), w.double(), b.double(), r.double(), "silu", dtype)
+    assert ((out[:M].cpu().double() - ref).abs() <= bound).all() and (out[M] == 7).all()
+    w, b = _rand((2 * N, K), dtype, 5, K ** -0.5), _rand((2 * N,), F32, 6)
+    ref, bound = O.glu(x.double(), w.double(), b.double(), "gelu", dtype)
+    assert ((B.glu(x.to(DEV), w.to(DEV), b.to(DEV)).cpu().double() - ref).abs() <= bound).all()
