@@ -92,7 +92,9 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, const AttnParts& pa
 }
 
 // 128 query rows per workgroup, 32 per wave; keys and values pass through LDS in tiles of 64 while the next tile is on its way in registers.
-// Two waves a SIMD as long as their registers suffice; wide heads give up the tile on its way for that.
+// Two waves a SIMD at least, as long as their registers suffice (up to 64 channels the compiler needs 105 to 145 and leaves room for three); wide heads give up the
+// tile on its way for that.  What bounds it, at 2 x 10 x 4096 x 4096 x 64 (128 us): 640 workgroups are two or three a unit, 1.75 waves a SIMD on the mean; the vector unit
+// is busy 48 % of the time (180 instructions a 64x32 tile beside its 16 MFMAs), the MFMAs 27 %, LDS 21 %.
 template <typename E, int DP> constexpr int attention_waves() { return DP <= (sizeof(E) == 2 ? 10 : 5) ? 2 : 1; }
 template <typename E, int DP> constexpr int attention_few_waves() { return DP <= 4 ? 2 : 1; }
 template <typename E, int DP> constexpr bool attention_ahead() { return sizeof(E) == 2 && DP <= 8; }
@@ -195,7 +197,8 @@ attention_kernel(AttnArgs a, AttnParts parts, int row_tiles, int nsplit, int tot
 
 // At most 32 query rows a key head (one token of each query head that shares it, say): the four waves of a workgroup take different keys for the same
 // rows and are joined in LDS.  Bound by reading keys and values: each wave streams tiles of its own through LDS of its own, without a barrier in the loop,
-// with the next tile in flight (128 KB a compute unit at 128 channels).
+// with the next tile in flight (128 KB a compute unit at 128 channels).  8 x 15000 keys of 8 x 128 channels, bf16: 3.8 TB/s on those that are valid.  One wave a SIMD from
+// 80 channels on; above 96 the registers spill all the same, 36 bytes a lane at 128 channels, 60 at 160, 172 at 256.
 template <typename E, int DP> struct AttnFew {
     using T = AttnTile<E, DP>;
     static constexpr int SUBS = T::ES == 2 && DP <= 10 ? 2 : 1, KEYS = 32 * SUBS;

@@ -20,7 +20,8 @@ struct BackwardParts {
 template <typename E, int DP> constexpr int dq_waves() { return DP <= (sizeof(E) == 2 ? 5 : 4) ? 2 : 1; }
 template <typename E, int DP> constexpr int backward_waves() { return DP <= (sizeof(E) == 2 ? 6 : 4) ? 2 : 1; }
 // Two-byte types keep two tiles in LDS and one on its way, except where its registers and addresses cost more than it hides: us with / without, for
-// 2 x 8 x 1024 x 1024 x D (128: 2 x 8 x 2048 x 2048): D 96 57 / 58, 128 187 / 173, 160 94 / 99, 256 366 / 153 (registers spill).  fp32's tiles are too large for it.
+// 2 x 8 x 1024 x 1024 x D in bf16 (128: 2 x 8 x 2048 x 2048): D 96 57 / 58, 128 187 / 173, 160 94 / 99, 256 366 / 153 (648 bytes a lane spilled; without it 148 to 312 are
+// still).  fp32's tiles are too large for it.
 template <typename E, int DP> constexpr bool backward_ahead() { return sizeof(E) == 2 && (DP <= 6 || DP == 10); }
 
 // fp16 ends at 65504 and loses bits below 6e-5, and the gradients of the scores may lie beyond either where the results do not.  They become an operand times
@@ -463,8 +464,9 @@ int backward_ranges(int B, int Sq, int Skv, int H, int Hkv, int D, int dt) {
 }
 // Whether workgroups own 128 rows, 32 a wave, rather than 64.  Tiles then pass through LDS half as often and no halves are added, but a workgroup has twice
 // the work, which takes it 1.75 times as long (fp32, bound by its MFMAs, 1.95): taken where that beats the rounds in which the chip runs twice as many
-// workgroups of 64.  us with 64 / 128 (B x H x Sq x Skv x D, bf16): 4 x 10 x 1024 x 154 x 64 (dq) 40 / 37, 1 x 10 x 4096 x 4096 x 64 277 / 248,
-// 4 x 16 x 1024 x 1024 x 80 153 / 121, 2 x 8 x 2048 x 2048 x 128 238 / 187; 4 x 8 x 1024 x 1024 x 80 73 / 84.
+// workgroups of 64.  us of both kernels with 64 / 128 (B x H x Sq x Skv x D, bf16): 1 x 10 x 4096 x 4096 x 64 280 / 250, 4 x 16 x 1024 x 1024 x 80 140 / 118,
+// 2 x 8 x 2048 x 2048 x 128 263 / 171, 4 x 8 x 1024 x 1024 x 80 71 / 83, 2 x 8 x 1024 x 1024 x 160 85 / 118; 4 x 10 x 1024 x 154 x 64 38.8 / 38.0, and 35.3 by the rule, which asks
+// for each of them; fp32 4 x 8 x 1024 x 1024 x 80 396 / 355, 2 x 8 x 1024 x 1024 x 160 366 / 457.
 bool own_wide(long long heads, int rows, int waves, bool f32) {
     const long long slots = 256 * waves, narrow = heads * (((long long)rows + 63) / 64), wide = heads * (((long long)rows + 127) / 128);
     return (double)((narrow + slots - 1) / slots) > (f32 ? 1.95 : 1.75) * (double)((wide + slots - 1) / slots);

@@ -78,7 +78,8 @@ bool product_dims_ok(int M, int N, int K, int halves) {
     return gemm_dims_ok(M, W, K) && gemm_dims_ok(M, K, W) && gemm_dims_ok(W, K, M);
 }
 
-// one call for both backward passes: `halves` rows of w per output column
+// One call for both backward passes: `halves` rows of w per output column.  dz is stored in the type of dy, because it is an operand of the two products after it and a matrix
+// instruction takes both operands in one type; a rounding more than its own in dx and dw (bf16, 4096 x 640 x 2560: error against 64 bits 2.3e-3 where one rounding is 1.7e-3).
 int products_backward(const void* x, const void* w, const float* bias, const void* dy, void* dx, void* dw, float* dbias, int M, int N, int K, long long ldx,
                       long long lddy, long long lddx, int dt, int act, int halves, void* workspace, size_t workspace_bytes, void* stream) {
     if (!x || !w || !dy || (!dx && !dw && !dbias)) return WINO_ERR_NULL;
