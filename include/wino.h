@@ -426,7 +426,8 @@ int wino_glu_backward(const void *x, const void *w, const float *bias, const voi
  *     s_ij = scale * sum_d q[b][i][h][d] * k[b][j][h'][d],   p_i = softmax over the valid j,   o[b][i][h] = sum_j p_ij v[b][j][h']
  *   with h' = h / (H / Hkv): neighbouring query heads share a key head.  Key j of batch row b is valid if j < kv_len[b] and
  *   key_mask[b][j] != 0 (device arrays, either may be NULL; a length outside [0, Skv] counts as the nearer end).  A batch row without
- *   a valid key gives o = 0 and lse = -infinity.  What k and v hold at other keys is never read.
+ *   a valid key gives o = 0, lse = -infinity and zero gradients.  What k and v hold at other keys is never read.  (A query whose scores are
+ *   -infinity at every valid key gives o = 0 and lse = -infinity too, but NaN gradients: the definition has no value there.)
  *   lse[b][h][i] = log sum_j exp(s_ij), fp32 [B][H][Sq]; NULL where no backward pass follows.
  * Tensors are [batch][position][head][D] with strides of their own in elements (a slice of a packed q,k,v product is read in place);
  * D is contiguous, a multiple of 8, at most 256 (fp32: 160).  Strides are not negative and multiples of 16 bytes; those of outputs
