@@ -29,8 +29,8 @@ template <typename E, int DP> constexpr bool backward_ahead() { return sizeof(E)
 // that factor too.  e falls when a value passes 2^15, to where the column's largest so far is between 2^7 and 2^8: once or twice a column.  The first e cannot take
 // a value out of fp32: |ds| < 2^42, by fp16's own range.  Softmax weights are at most 1 and take a fixed 2^12, with which 2^-26 is still a normal number.
 // Heads of more than 160 channels have no registers left for the branch: they find the largest value in a pass of its own and keep one e (2 x 8 x 1024 x 1024 x
-// 256: 233 us; 465 with the branch, which spills).  us without / with factors: 4 x 10 x 1024 x 154 x 64 33.8 / 35.1, 4 x 8 x 1024 x 1024 x 80 71 / 75,
-// 2 x 10 x 4096 x 4096 x 64 436 / 467, 2 x 8 x 2048 x 2048 x 128 171 / 186, 2 x 8 x 1024 x 1024 x 256 152 / 233.
+// 256: 234 us; 465 with the branch, which spills).  us without / with factors: 4 x 10 x 1024 x 154 x 64 33.6 / 34.8, 4 x 8 x 1024 x 1024 x 80 73 / 77 (20 to 44
+// bytes a lane spilled), 2 x 10 x 4096 x 4096 x 64 451 / 476, 2 x 8 x 2048 x 2048 x 128 171 / 180, 2 x 8 x 1024 x 1024 x 256 152 / 234.
 template <typename E> constexpr bool short_range() { return std::is_same_v<E, __half>; }
 template <typename E, int DP> constexpr bool two_passes() { return short_range<E>() && DP > 10; }
 constexpr int kWeightPower = 12;
@@ -209,15 +209,29 @@ attention_dq_kernel(AttnArgs a, float* delta, int row_tiles, int total, int per_
                     power.look(dp);
                     continue;
                 }
-                if constexpr (short_range<E>() && !TWICE) power.settle<T::NV>(dp, acc, rest, true);
+                // (with a branch for the factors: the mean's products run beside it)
+                constexpr bool SETTLE = short_range<E>() && !TWICE;
+                u32x4_t keys[T::ST][T::NV];
+                if constexpr (SETTLE) {
+#pragma unroll
+                    for (int st = 0; st < T::ST; ++st) {
+                        const u32x4_t wp = T::weights(s, st);
+#pragma unroll
+                        for (int d = 0; d < T::NV; ++d) {
+                            keys[st][d] = T::across(tk, 32 * h, st, d, places);
+                            Mma<E>::run(keys[st][d], wp, acc[T::NV + d]);
+                        }
+                    }
+                    power.settle<T::NV>(dp, acc, rest, true);
+                }
 #pragma unroll
                 for (int st = 0; st < T::ST; ++st) {
                     const u32x4_t w = T::weights(dp, st), wp = MEAN ? T::weights(s, st) : w;
 #pragma unroll
                     for (int d = 0; d < T::NV; ++d) {
-                        const u32x4_t keys = T::across(tk, 32 * h, st, d, places);
-                        Mma<E>::run(keys, w, acc[d]);
-                        if constexpr (MEAN) Mma<E>::run(keys, wp, acc[T::NV + d]);
+                        if constexpr (!SETTLE) keys[st][d] = T::across(tk, 32 * h, st, d, places);
+                        Mma<E>::run(keys[st][d], w, acc[d]);
+                        if constexpr (MEAN && !SETTLE) Mma<E>::run(keys[st][d], wp, acc[T::NV + d]);
                     }
                 }
             }
@@ -364,14 +378,23 @@ attention_dkv_kernel(AttnArgs a, BackwardParts parts, int key_tiles, int nsplit,
                         power.look(dp);
                         continue;
                     }
-                    float none = 0.f;
-                    if constexpr (short_range<E>() && !TWICE) power.settle<T::NV>(dp, acc, none, key_on);
+                    constexpr bool SETTLE = short_range<E>() && !TWICE;                  // as above, with dv's products
+                    if constexpr (SETTLE) {
+#pragma unroll
+                        for (int st = 0; st < T::ST; ++st) {
+                            const u32x4_t wp = T::weights(s, st);
+#pragma unroll
+                            for (int d = 0; d < T::NV; ++d) Mma<E>::run(T::across(to, 32 * h, st, d, places), wp, acc[T::NV + d]);
+                        }
+                        float none = 0.f;
+                        power.settle<T::NV>(dp, acc, none, key_on);
+                    }
 #pragma unroll
                     for (int st = 0; st < T::ST; ++st) {
                         const u32x4_t wp = T::weights(s, st), wd = T::weights(dp, st);
 #pragma unroll
                         for (int d = 0; d < T::NV; ++d) {
-                            Mma<E>::run(T::across(to, 32 * h, st, d, places), wp, acc[T::NV + d]);
+                            if constexpr (!SETTLE) Mma<E>::run(T::across(to, 32 * h, st, d, places), wp, acc[T::NV + d]);
                             Mma<E>::run(T::across(tq, 32 * h, st, d, places), wd, acc[d]);
                         }
                     }
