@@ -364,8 +364,8 @@ int wino_i8_batched_gemm(const void *Uq, const float *dU, const void *Vq, const 
                          int K, int C, int T, int block_shape, void *stream);
 
 /*
- * The operators of the transformer block that stands between two residual blocks of a Stable-Diffusion UNet, on channel-last
- * activations (a [N][H][W][C] tensor is M = N*H*W rows of C features as it stands): matrix products with bias, activation and
+ * The matrix and attention operators (not the LayerNorms) of the transformer block that stands between two residual blocks of a
+ * Stable-Diffusion UNet, on channel-last activations (a [N][H][W][C] tensor is M = N*H*W rows of C features as it stands): matrix products with bias, activation and
  * residual in their epilogue, the gated feed-forward product, and attention to an encoder's states, each with its backward pass.
  * The paper defines none of them; the textbook definitions apply.  Storage types, accumulation, streams, alignment of pointers,
  * determinism and errors as above.  Sums, softmax statistics and bias gradients are fp32; a result is rounded once to `dtype`.

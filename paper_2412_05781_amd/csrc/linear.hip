@@ -339,6 +339,7 @@ long long gemm_most_tops(int M, int N) { return 4 * (((long long)M + 63) / 64 + 
 // ranges' sums written and read.  Two-byte products with enough tiles of 128x128 are not cut at all.  The ranges together may reach a larger block (launch_shape), which is
 // only faster.  us, one range / as counted / as counted in 64x64 (M x K x N, fp16): 90 x 5120 x 320 22.5 / 9.0 / 9.0, 256 x 2560 x 1280 13.2 / 12.3 / 12.0, 512 x 10240 x 1280
 // 42.6 / 27.8 / 34.8, 1000 x 5120 x 1280 32.0 / 30.2 / 32.8; odd 90 x 2563 x 320 41.6 / 18.7, 1000 x 5123 x 1280 85.8 / 58.9; fp32 2028 x 2560 x 320 52.0 / 38.5.
+// The gated product is not cut: few tiles of it wait 6 us per 1000 of the reduction (64 x 5120 x 2 x 1280 33 us).
 int gemm_ranges(int M, int N, int K, int dt) {
     auto tiles = [&](int n, int m) { return (((long long)N + n - 1) / n) * (((long long)M + m - 1) / m); };
     const bool f32 = dt == DT_F32;

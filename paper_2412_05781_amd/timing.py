@@ -256,10 +256,11 @@ def _block_row(name, run, nbytes, flops, framework=None):
     print(line, flush=True)
 
 
-def cmd_transformer(_):
+def cmd_transformer(a):
     F = torch.nn.functional
-    dt = B.DTYPE_OF[DT]
-    r = lambda *shape, std=1.0: (torch.randn(*shape, device=DEV) * std).to(DT)
+    td = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}[a.dtype]
+    dt, es = B.DTYPE_OF[td], td.itemsize
+    r = lambda *shape, std=1.0: (torch.randn(*shape, device=DEV) * std).to(td)
     space = lambda n: torch.empty(n, dtype=torch.uint8, device=DEV) if n else None
     n = 3
     # the UNet levels of one 512x512 image and one 1024x1024 image, guidance batch: tokens, channels, heads, channels a head
@@ -268,23 +269,23 @@ def cmd_transformer(_):
         print(f"-- {N} x {HW} tokens of {C} channels, {H} heads", flush=True)
         xs, ys, hs = [r(M, C) for _ in range(n)], [r(M, C) for _ in range(n)], [r(M, KV) for _ in range(n)]
         w, b, wg, bg, wd = r(C, C, std=C ** -0.5), torch.zeros(C, device=DEV), r(2 * KV, C, std=C ** -0.5), torch.zeros(2 * KV, device=DEV), r(C, KV, std=KV ** -0.5)
-        b16, bg16 = b.to(DT), bg.to(DT)
+        b16, bg16 = b.to(td), bg.to(td)
         ws = space(max(B.wino_linear_workspace_bytes(M, C, C, dt), B.wino_linear_workspace_bytes(M, C, KV, dt)))
-        _block_row("linear C -> C, bias, residual", lambda i: B.wino_linear(xs[i % n], w, b, ys[i % n], 0, ys[i % n], ws), 3 * M * C * 2 + C * C * 2, 2.0 * M * C * C,
+        _block_row("linear C -> C, bias, residual", lambda i: B.wino_linear(xs[i % n], w, b, ys[i % n], 0, ys[i % n], ws), (3 * M * C + C * C) * es, 2.0 * M * C * C,
                    lambda i: F.linear(xs[i % n], w, b16) + ys[i % n])
-        _block_row("gated feed-forward C -> 2 x 4C", lambda i: B.wino_glu(xs[i % n], wg, bg, hs[i % n]), (M * C + M * KV + 2 * KV * C) * 2, 4.0 * M * C * KV,
+        _block_row("gated feed-forward C -> 2 x 4C", lambda i: B.wino_glu(xs[i % n], wg, bg, hs[i % n]), (M * C + M * KV + 2 * KV * C) * es, 4.0 * M * C * KV,
                    lambda i: (lambda u, g: u * F.gelu(g))(*F.linear(xs[i % n], wg, bg16).chunk(2, 1)))
-        _block_row("linear 4C -> C, bias, residual", lambda i: B.wino_linear(hs[i % n], wd, b, ys[i % n], 0, ys[i % n], ws), (2 * M * C + M * KV + C * KV) * 2, 2.0 * M * C * KV,
+        _block_row("linear 4C -> C, bias, residual", lambda i: B.wino_linear(hs[i % n], wd, b, ys[i % n], 0, ys[i % n], ws), (2 * M * C + M * KV + C * KV) * es, 2.0 * M * C * KV,
                    lambda i: F.linear(hs[i % n], wd, b16) + ys[i % n])
         dx, dw, db = torch.empty_like(xs[0]), torch.empty_like(wg), torch.empty_like(bg)
         wsb = space(B.wino_glu_backward_workspace_bytes(M, KV, C, dt, B.WINO_ACT_GELU))
         _block_row("gated feed-forward, gradients", lambda i: B.wino_glu_backward(xs[i % n], wg, bg, hs[i % n], dx, dw, db, workspace=wsb),
-                   (2 * M * C + M * KV + 4 * KV * C) * 2, 12.0 * M * C * KV)
+                   (2 * M * C + M * KV + 4 * KV * C) * es, 12.0 * M * C * KV)
         for S, what in ((L, "attention to 77 states"), (HW, "attention among the tokens")):
             q, k, v = [r(N, HW, H, D) for _ in range(n)], [r(N, S, H, D) for _ in range(n)], [r(N, S, H, D) for _ in range(n)]
             o, lse, do = torch.empty_like(q[0]), torch.empty((N, H, HW), device=DEV), r(N, HW, H, D)
             wsa = space(B.wino_attention_workspace_bytes(N, HW, S, H, H, D, dt))
-            nbytes, flops = 4 * N * (HW + S) * C, 4.0 * N * HW * S * C
+            nbytes, flops = 2 * N * (HW + S) * C * es, 4.0 * N * HW * S * C
             _block_row(what, lambda i: B.wino_attention(q[i % n], k[i % n], v[i % n], o, workspace=wsa), nbytes, flops)
             B.wino_attention(q[0], k[0], v[0], o, lse, workspace=wsa)
             dq, dk, dv = torch.empty_like(q[0]), torch.empty_like(k[0]), torch.empty_like(v[0])
@@ -295,6 +296,7 @@ def cmd_transformer(_):
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("what", choices=["fused", "upsample", "flavours", "direct", "half-product", "variants", "int8", "transformer"])
+    ap.add_argument("--dtype", choices=["f16", "bf16", "f32"], default="f16", help="storage type of the transformer block's operators")
     a = ap.parse_args(argv)
     if not torch.cuda.is_available():
         print("timing: no GPU visible", file=sys.stderr)
