@@ -125,3 +125,34 @@ def test_few_rows_and_long_reductions(M, K, N, dtype):
     w, b = _rand((2 * N, K), dtype, 5, K ** -0.5), _rand((2 * N,), F32, 6)
     ref, bound = O.glu(x.double(), w.double(), b.double(), "gelu", dtype)
     assert ((B.glu(x.to(DEV), w.to(DEV), b.to(DEV)).cpu().double() - ref).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("M,K,N", [(3, 64, 40), (64, 5120, 320), (200, 4096, 328), (257, 320, 328), (2100, 328, 640), (300, 75, 131), (3600, 1544, 520)])
+def test_residual_in_place(M, K, N, dtype):
+    """The output over its own residual, in every kernel that finishes a product: bit for bit what two tensors give."""
+    x, w, b, r = (_rand(s, t, i, f).to(DEV) for s, t, i, f in (((M, K), dtype, 1, 1.0), ((N, K), dtype, 2, K ** -0.5), ((N,), F32, 3, 1.0), ((M, N), dtype, 4, 1.0)))
+    n = B.wino_linear_workspace_bytes(M, N, K, B.DTYPE_OF[dtype], B.WINO_ACT_GELU)
+    apart, wide = torch.empty_like(r), torch.full((M, N + 16), 7.0, dtype=dtype, device=DEV)
+    B.wino_linear(x, w, b, apart, B.WINO_ACT_GELU, r, _space(n) if n else None)
+    wide[:, :N] = r
+    B.wino_linear(x, w, b, r, B.WINO_ACT_GELU, r, _space(n) if n else None)
+    B.wino_linear(x, w, b, wide[:, :N], B.WINO_ACT_GELU, wide[:, :N], _space(n) if n else None)
+    assert torch.equal(r, apart) and torch.equal(wide[:, :N], apart) and (wide[:, N:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("H,Sq", [(32, 1), (33, 1), (64, 1), (11, 3), (128, 2)])
+def test_many_query_heads_of_one_key_head(H, Sq, dtype):
+    """Either side of the 32 rows a key head that one wave holds, with ranges of the keys, and their gradients."""
+    Bn, Skv, D = 2, 1700, 64
+    q, do = _rand((Bn, Sq, H, D), dtype, 1, 1.5), _rand((Bn, Sq, H, D), dtype, 2)
+    k, v = _rand((Bn, Skv, 1, D), dtype, 3), _rand((Bn, Skv, 1, D), dtype, 4)
+    lens = [Skv, 900]
+    valid = torch.arange(Skv)[None] < torch.tensor(lens)[:, None]
+    kw = dict(kv_len=torch.tensor(lens, dtype=torch.int32, device=DEV))
+    o, lse = _attention(q, k, v, valid, (H, Sq, dtype), **kw)
+    got = B.attention_backward(q.to(DEV), k.to(DEV), v.to(DEV), o, lse, do.to(DEV), **kw)
+    for name, g, (ref, bound) in zip(("dq", "dk", "dv"), got, O.attention_backward(q.double(), k.double(), v.double(), valid, D ** -0.5, do.double(), dtype)):
+        assert ((g.cpu().double() - ref).abs() <= bound).all(), (name, H, Sq)
+    assert (got[1][1, 900:] == 0).all() and (got[2][1, 900:] == 0).all()
